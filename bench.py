@@ -351,10 +351,10 @@ def kernel_sources_sha256():
 # sources reports traffic = null (tests/test_bench_line.py fails until the capture is refreshed or
 # cleared).
 NCU_TRAFFIC = {
-    "sources": "ec1253670ed84ca89c42f748dcac88b228d8c60154f9681673f721f452b00cab",
+    "sources": None,
     "captured_tokens": 16384,
-    "sparse_bytes_per_launch": 497992978,     # mean over the 14 sparse GEMM launches of one step
-    "dense_bytes_per_launch": 742438510,     # mean over the 7 weight-gradient launches of one step
+    "sparse_bytes_per_launch": None,     # mean over the 14 sparse GEMM launches of one step
+    "dense_bytes_per_launch": None,     # mean over the 7 weight-gradient launches of one step
 }
 
 

@@ -60,6 +60,9 @@ typedef enum {
     SLOPE_ERR_TIMEOUT = 6           /* a bounded device-side wait ran out      */
 } slope_status_t;
 
+/* Element types of the calls that take more than bf16.  SLOPE_Q8: a checkpoint (see slope_checkpoint_store). */
+typedef enum { SLOPE_BF16 = 0, SLOPE_F32 = 1, SLOPE_Q8 = 2 } slope_type_t;
+
 /* Buffer sizes in bytes of the compressed format of a [rows x cols] matrix. */
 size_t slope_values_bytes(int rows, int cols);
 size_t slope_meta_bytes(int rows, int cols);
@@ -286,6 +289,69 @@ slope_status_t slope_dense_linear_bwd_dw(const void* dY, const void* X, int b, i
 size_t slope_adapter_dl_noalloc_max_scratch_bytes(void);
 slope_status_t slope_adapter_dl_noalloc(const void* X, const void* dT, int b, int d_in, int r,
                                         void* dL, void* stream);
+
+/*
+ * 8-bit checkpoints of activations: what a training step keeps of X between the forward and the backward pass, 33 / 64 of the bytes
+ * of bf16.  (The paper counts weights, gradients and optimizer states only; activations stay dense.)  Of a matrix
+ * [rows x cols], cols a multiple of 32, each block of 32 consecutive values of a row is stored as 32 signed bytes times one power
+ * of two 2^k: k the smallest integer for which the block's largest magnitude is at most 127.5 * 2^k, within
+ * [-126, 121]; code = x / 2^k rounded half to even and held in [-127, 127].  A value that is read back is code * 2^k: off by at
+ * most 2^k / 2 (below 2^-126: absolutely), and exact in bf16.  A block with an infinity or a NaN reads back as NaN.
+ * Buffer: the rows * cols codes, row-major, then rows * cols / 32 bytes k + 127 (255 for a block of NaN).
+ *   slope_checkpoint_store   checkpoint of X (x_type SLOPE_BF16 or SLOPE_F32)
+ *   slope_checkpoint_load    X (bf16 or fp32) from a checkpoint
+ */
+size_t slope_checkpoint_bytes(int rows, int cols);
+slope_status_t slope_checkpoint_store(const void* X, int x_type, int rows, int cols, void* checkpoint, void* stream);
+slope_status_t slope_checkpoint_load(const void* checkpoint, int rows, int cols, void* X, int x_type, void* stream);
+
+/*
+ * Layer norm, what stands in front of the sparse layers of GPT-2, OPT and BERT (Sec. "Experiment Setup"):
+ *   h = X (+ residual),  m = mean(h),  s = 1 / sqrt(mean((h - m)^2) + eps),  Y = (h - m) s gamma + beta
+ * row by row; X, H [b x d] of x_type (SLOPE_BF16 or SLOPE_F32), residual and Y bf16, gamma and beta [d] of p_type (bf16 or fp32; NULL:
+ * ones, zeros), mean and rstd (s) fp32 [b], all sums fp32.  d is a multiple of 8, at most 16384; b any.
+ *   residual    a sub-layer's output that is added first, or NULL
+ *   H           receives the sum (rounded to x_type, and it is the rounded one that is normalised); NULL: not kept.  H may be X or,
+ *               where x_type is bf16, residual.  Without a residual H must be NULL.
+ *   mean, rstd  for the backward pass; both NULL at inference
+ *   H_ckpt      checkpoint of h (of X without a residual), for slope_layer_norm_bwd, or NULL     } d a multiple of 32
+ *   Y_ckpt      checkpoint of Y, for the weight gradients of the layers behind it, or NULL        }
+ * Otherwise outputs must not overlap inputs or one another.  A row with an infinity or a NaN has NaN statistics and outputs.
+ */
+slope_status_t slope_layer_norm_fwd(const void* X, int x_type, const void* residual, const void* gamma, const void* beta, int p_type,
+                                    int b, int d, float eps, void* H, void* Y, void* mean, void* rstd,
+                                    void* H_ckpt, void* Y_ckpt, void* stream);
+
+/*
+ * Its backward pass: with x = (h - m) s and g = dY gamma,
+ *   dX = s (g - mean(g) - x mean(g x)) (+ dH),   dgamma = sum over the rows of dY x,   dbeta = sum over the rows of dY.
+ * H is the normalised stream: bf16, fp32 or its checkpoint (h_type SLOPE_Q8; the statistics are still those of the stream itself).
+ * dY bf16; dX and dH (the gradient that reaches h past the layer norm, or NULL) of dx_type (bf16 or fp32); dgamma, dbeta [d] of p_type, each NULL if not
+ * wanted.  dX may be dH or, where dx_type is bf16, dY; otherwise outputs must not overlap inputs or one another.  The sums over the rows have a
+ * fixed order.  `workspace`: device scratch of at least slope_layer_norm_bwd_workspace_bytes() bytes (NULL if that is 0, or if neither dgamma nor
+ * dbeta is wanted).
+ */
+size_t slope_layer_norm_bwd_workspace_bytes(int b, int d);
+slope_status_t slope_layer_norm_bwd(const void* dY, const void* H, int h_type, const void* mean, const void* rstd,
+                                    const void* gamma, int p_type, const void* dH, int b, int d,
+                                    void* dX, int dx_type, void* dgamma, void* dbeta,
+                                    void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The weight gradients with X from its checkpoint: the outputs of slope_linear_bwd_dw_masked, slope_linear_bwd_dw_adapter and
+ * slope_dense_linear_bwd_dw for the matrix that the checkpoint reads back as (rounded once, sums in an order of their own).
+ * `workspace`: device scratch of at least slope_bwd_dw_q8_workspace_bytes() bytes (r = 0: no adapters; NULL if that is 0).
+ */
+size_t slope_bwd_dw_q8_workspace_bytes(int b, int d_out, int d_in, int r);
+slope_status_t slope_linear_bwd_dw_masked_q8(const void* dY, const void* X_ckpt, int b, int d_out, int d_in,
+                                             const void* mask1_bits, void* dWc_vals,
+                                             void* workspace, size_t workspace_bytes, void* stream);
+slope_status_t slope_linear_bwd_dw_adapter_q8(const void* dY, const void* X_ckpt, const void* T, const void* dT,
+                                              int b, int d_out, int d_in, int r,
+                                              const void* mask1_bits, void* dWc_vals, void* dL, void* dR,
+                                              void* workspace, size_t workspace_bytes, void* stream);
+slope_status_t slope_dense_linear_bwd_dw_q8(const void* dY, const void* X_ckpt, int b, int d_out, int d_in, void* dW,
+                                            void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Diagnostic: rewrite tensor-core-order metadata as canonical metadata

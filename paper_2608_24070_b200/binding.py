@@ -35,6 +35,10 @@ EXPORTS = (
     "slope_dense_linear_fwd", "slope_dense_linear_bwd_dx", "slope_dense_linear_bwd_dw", "slope_mask_difference",
     "slope_linear_fwd_adapter", "slope_prune_24_double",
     "slope_bwd_dw_adapter_workspace_bytes", "slope_linear_bwd_dw_adapter", "slope_kernel_clock_mhz",
+    "slope_checkpoint_bytes", "slope_checkpoint_store", "slope_checkpoint_load",
+    "slope_layer_norm_fwd", "slope_layer_norm_bwd_workspace_bytes", "slope_layer_norm_bwd",
+    "slope_bwd_dw_q8_workspace_bytes", "slope_linear_bwd_dw_masked_q8", "slope_linear_bwd_dw_adapter_q8",
+    "slope_dense_linear_bwd_dw_q8",
 )
 
 
@@ -96,6 +100,18 @@ def lib() -> ctypes.CDLL:
         L.slope_apply_mask.restype = ci
         L.slope_selftest_wait_timeout.argtypes = [ctypes.c_uint, vp, vp]
         L.slope_selftest_wait_timeout.restype = ci
+        for name, args in {
+            "slope_checkpoint_store": [vp, ci, ci, ci, vp, vp],
+            "slope_checkpoint_load": [vp, ci, ci, vp, ci, vp],
+            "slope_layer_norm_fwd": [vp, ci, vp, vp, vp, ci, ci, ci, ctypes.c_float, vp, vp, vp, vp, vp, vp, vp],
+            "slope_layer_norm_bwd": [vp, vp, ci, vp, vp, vp, ci, vp, ci, ci, vp, ci, vp, vp, vp, sz, vp],
+            "slope_linear_bwd_dw_masked_q8": [vp, vp, ci, ci, ci, vp, vp, vp, sz, vp],
+            "slope_linear_bwd_dw_adapter_q8": [vp, vp, vp, vp, ci, ci, ci, ci, vp, vp, vp, vp, vp, sz, vp],
+            "slope_dense_linear_bwd_dw_q8": [vp, vp, ci, ci, ci, vp, vp, sz, vp],
+        }.items():
+            getattr(L, name).argtypes, getattr(L, name).restype = args, ci
+        for name, count in {"slope_checkpoint_bytes": 2, "slope_layer_norm_bwd_workspace_bytes": 2, "slope_bwd_dw_q8_workspace_bytes": 4}.items():
+            getattr(L, name).argtypes, getattr(L, name).restype = [ci] * count, sz
         L.slope_poll_status.argtypes = [vp]
         L.slope_kernel_clock_mhz.argtypes = [ci, vp, ctypes.POINTER(ctypes.c_double)]
         L.slope_kernel_clock_mhz.restype = ci
@@ -276,6 +292,64 @@ def slope_dense_linear_bwd_dw(dY, X, dW):
         _check("slope_dense_linear_bwd_dw", st)
 
 
+def slope_checkpoint_bytes(rows: int, cols: int) -> int:
+    return int(lib().slope_checkpoint_bytes(rows, cols))
+
+
+def slope_checkpoint_store(X, checkpoint):
+    """Checkpoint (``alloc_checkpoint``) of a bf16 or fp32 matrix: 8-bit codes, one power of two per 32 values of a row."""
+    st = (_native or _calls()).slope_checkpoint_store(X, checkpoint)
+    if st:
+        _check("slope_checkpoint_store", st)
+
+
+def slope_checkpoint_load(checkpoint, X):
+    """The bf16 or fp32 matrix that a checkpoint stands for."""
+    st = (_native or _calls()).slope_checkpoint_load(checkpoint, X)
+    if st:
+        _check("slope_checkpoint_load", st)
+
+
+def slope_layer_norm_fwd(X, gamma, beta, eps, Y, mean=None, rstd=None, residual=None, H=None, H_ckpt=None, Y_ckpt=None):
+    """Y = layer norm of X (+ residual); optionally the sum H, the statistics and checkpoints of H (of X without a residual) and Y."""
+    st = (_native or _calls()).slope_layer_norm_fwd(X, gamma, beta, eps, Y, mean, rstd, residual, H, H_ckpt, Y_ckpt)
+    if st:
+        _check("slope_layer_norm_fwd", st)
+
+
+def slope_layer_norm_bwd_workspace_bytes(b: int, d: int) -> int:
+    return int(lib().slope_layer_norm_bwd_workspace_bytes(b, d))
+
+
+def slope_layer_norm_bwd(dY, H, mean, rstd, gamma, dX, dgamma=None, dbeta=None, workspace=None, dH=None):
+    """dX (+ dH), dgamma and dbeta; H is the normalised stream, bf16, fp32 or a checkpoint of it."""
+    st = (_native or _calls()).slope_layer_norm_bwd(dY, H, mean, rstd, gamma, dX, dgamma, dbeta, workspace, dH)
+    if st:
+        _check("slope_layer_norm_bwd", st)
+
+
+def slope_bwd_dw_q8_workspace_bytes(b: int, d_out: int, d_in: int, r: int = 0) -> int:
+    return int(lib().slope_bwd_dw_q8_workspace_bytes(b, d_out, d_in, r))
+
+
+def slope_linear_bwd_dw_masked_q8(dY, X_ckpt, mask1_bits, dWc_vals, workspace=None):
+    st = (_native or _calls()).slope_linear_bwd_dw_masked_q8(dY, X_ckpt, mask1_bits, dWc_vals, workspace)
+    if st:
+        _check("slope_linear_bwd_dw_masked_q8", st)
+
+
+def slope_linear_bwd_dw_adapter_q8(dY, X_ckpt, T, dT, mask1_bits, dWc_vals, dL, dR, workspace=None):
+    st = (_native or _calls()).slope_linear_bwd_dw_adapter_q8(dY, X_ckpt, T, dT, mask1_bits, dWc_vals, dL, dR, workspace)
+    if st:
+        _check("slope_linear_bwd_dw_adapter_q8", st)
+
+
+def slope_dense_linear_bwd_dw_q8(dY, X_ckpt, dW, workspace=None):
+    st = (_native or _calls()).slope_dense_linear_bwd_dw_q8(dY, X_ckpt, dW, workspace)
+    if st:
+        _check("slope_dense_linear_bwd_dw_q8", st)
+
+
 def slope_mask_difference(mask_a, mask_b, count_out):
     rows, mrow = mask_a.shape
     _check("slope_mask_difference", lib().slope_mask_difference(_ptr(mask_a), _ptr(mask_b), rows, mrow * 8,
@@ -328,6 +402,14 @@ def alloc_compressed(rows: int, cols: int, device="cuda"):
     meta = torch.empty(slope_meta_bytes(rows, cols), dtype=torch.uint8, device=device)
     mask = torch.empty((rows, cols // 8), dtype=torch.uint8, device=device)
     return vals, meta, mask
+
+
+def alloc_checkpoint(rows: int, cols: int, device="cuda"):
+    """Caller-owned buffer of the 8-bit checkpoint of a [rows x cols] matrix (cols a multiple of 32)."""
+    nbytes = slope_checkpoint_bytes(rows, cols)
+    if nbytes == 0:
+        raise ValueError("a checkpoint has at least one row and a multiple of 32 columns")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
 def bf16_from_bits(bits, device="cuda") -> torch.Tensor:

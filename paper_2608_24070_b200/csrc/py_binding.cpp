@@ -11,6 +11,7 @@
 #include <dlfcn.h>
 
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -25,7 +26,9 @@ namespace {
     X(slope_prune_24) X(slope_double_prune) X(slope_prune_24_double) X(slope_linear_fwd) X(slope_linear_fwd_adapter)    \
     X(slope_linear_bwd_dx) X(slope_linear_bwd_dw_masked) X(slope_adapter_fwd_bwd) X(slope_linear_bwd_dw_adapter)        \
     X(slope_sparse_add) X(slope_update_sparse_matrix) X(slope_prune_nm) X(slope_double_prune_nm) X(slope_apply_mask)    \
-    X(slope_dense_linear_fwd) X(slope_dense_linear_bwd_dx) X(slope_dense_linear_bwd_dw)
+    X(slope_dense_linear_fwd) X(slope_dense_linear_bwd_dx) X(slope_dense_linear_bwd_dw)                                 \
+    X(slope_checkpoint_store) X(slope_checkpoint_load) X(slope_layer_norm_fwd) X(slope_layer_norm_bwd)                  \
+    X(slope_linear_bwd_dw_masked_q8) X(slope_linear_bwd_dw_adapter_q8) X(slope_dense_linear_bwd_dw_q8)
 
 // the library's entry points, looked up in the handle that binding.lib() loaded
 #define SLOPE_POINTER(name) decltype(&::name) p_##name = nullptr;
@@ -267,6 +270,129 @@ SLOPE_PY(slope_dense_linear_bwd_dw) {
         const at::Tensor &dY = a.matrix(), &X = a.matrix();
         void* dW = a.ptr();
         return call(p_slope_dense_linear_bwd_dw, dY.data_ptr(), X.data_ptr(), rows(dY), cols(dY), cols(X), dW);
+    });
+}
+
+// Calls that take tensors of several types and sizes that follow from one another: what does not fit is refused here, since the C ABI
+// sees addresses only.
+[[noreturn]] void refuse(PyObject* kind, const char* what) {
+    PyErr_SetString(kind, what);
+    throw Bad{};
+}
+int type_of(const at::Tensor& t) {
+    if (t.scalar_type() == at::kBFloat16) return SLOPE_BF16;
+    if (t.scalar_type() == at::kFloat) return SLOPE_F32;
+    refuse(PyExc_TypeError, "expected a bf16 or fp32 tensor");
+}
+void on_this_device(const at::Tensor& t) {
+    if (t.device().index() != c10::cuda::current_device()) refuse(PyExc_ValueError, "tensors must be on the current device");
+}
+// `t` (or None) as [rows x cols] of the type; rows = 0: a vector of cols
+void* checked(const at::Tensor* t, int64_t rows, int64_t cols, at::ScalarType type) {
+    if (!t) return nullptr;
+    if (t->scalar_type() != type) refuse(PyExc_TypeError, "tensor of the wrong type");
+    const bool fits = rows ? t->dim() == 2 && t->size(0) == rows && t->size(1) == cols : t->dim() == 1 && t->size(0) == cols;
+    if (!fits) refuse(PyExc_ValueError, "tensor of the wrong shape");
+    on_this_device(*t);
+    return t->data_ptr();
+}
+void* checked_checkpoint(const at::Tensor* t, int64_t rows, int64_t cols) {
+    if (!t) return nullptr;
+    if (t->scalar_type() != at::kByte || t->dim() != 1) refuse(PyExc_TypeError, "a checkpoint is a uint8 vector (alloc_checkpoint)");
+    if (t->numel() != rows * cols + rows * cols / 32) refuse(PyExc_ValueError, "checkpoint of another size");
+    on_this_device(*t);
+    return t->data_ptr();
+}
+at::ScalarType scalar(int type) { return type == SLOPE_F32 ? at::kFloat : at::kBFloat16; }
+struct Scratch {
+    void* at;
+    size_t bytes;
+    explicit Scratch(const at::Tensor* t) : at(t ? t->data_ptr() : nullptr), bytes(t ? t->nbytes() : 0) {
+        if (t) on_this_device(*t);
+    }
+};
+
+SLOPE_PY(slope_checkpoint_store) {
+    return guarded(args, n, [](Args& a) {
+        const at::Tensor& X = a.matrix();
+        const int type = type_of(X);
+        on_this_device(X);
+        void* ckpt = checked_checkpoint(&a.tensor(), X.size(0), X.size(1));
+        return call(p_slope_checkpoint_store, X.data_ptr(), type, rows(X), cols(X), ckpt);
+    });
+}
+SLOPE_PY(slope_checkpoint_load) {
+    return guarded(args, n, [](Args& a) {
+        const at::Tensor &ckpt = a.tensor(), &X = a.matrix();
+        const int type = type_of(X);
+        on_this_device(X);
+        return call(p_slope_checkpoint_load, checked_checkpoint(&ckpt, X.size(0), X.size(1)), rows(X), cols(X), X.data_ptr(), type);
+    });
+}
+SLOPE_PY(slope_layer_norm_fwd) {
+    return guarded(args, n, [](Args& a) {
+        const at::Tensor& X = a.matrix();
+        const at::Tensor *gamma = a.tensor_or_none(), *beta = a.tensor_or_none();
+        const float eps = a.number();
+        const at::Tensor& Y = a.tensor();
+        const at::Tensor *mean = a.tensor_or_none(), *rstd = a.tensor_or_none(), *residual = a.tensor_or_none(), *H = a.tensor_or_none(),
+                         *H_ckpt = a.tensor_or_none(), *Y_ckpt = a.tensor_or_none();
+        const int64_t b = X.size(0), d = X.size(1);
+        const int x_type = type_of(X), p_type = gamma ? type_of(*gamma) : beta ? type_of(*beta) : SLOPE_BF16;
+        on_this_device(X);
+        return call(p_slope_layer_norm_fwd, X.data_ptr(), x_type, checked(residual, b, d, at::kBFloat16), checked(gamma, 0, d, scalar(p_type)),
+                    checked(beta, 0, d, scalar(p_type)), p_type, rows(X), cols(X), eps, checked(H, b, d, scalar(x_type)),
+                    checked(&Y, b, d, at::kBFloat16), checked(mean, 0, b, at::kFloat), checked(rstd, 0, b, at::kFloat),
+                    checked_checkpoint(H_ckpt, b, d), checked_checkpoint(Y_ckpt, b, d));
+    });
+}
+SLOPE_PY(slope_layer_norm_bwd) {
+    return guarded(args, n, [](Args& a) {
+        const at::Tensor &dY = a.matrix(), &H = a.tensor(), &mean = a.tensor(), &rstd = a.tensor();
+        const at::Tensor* gamma = a.tensor_or_none();
+        const at::Tensor& dX = a.matrix();
+        const at::Tensor *dgamma = a.tensor_or_none(), *dbeta = a.tensor_or_none();
+        const Scratch ws(a.tensor_or_none());
+        const at::Tensor* dH = a.tensor_or_none();
+        const int64_t b = dY.size(0), d = dY.size(1);
+        const int h_type = H.scalar_type() == at::kByte ? static_cast<int>(SLOPE_Q8) : type_of(H), dx_type = type_of(dX);
+        const int p_type = gamma ? type_of(*gamma) : dgamma ? type_of(*dgamma) : dbeta ? type_of(*dbeta) : SLOPE_BF16;
+        return call(p_slope_layer_norm_bwd, checked(&dY, b, d, at::kBFloat16),
+                    h_type == SLOPE_Q8 ? checked_checkpoint(&H, b, d) : checked(&H, b, d, scalar(h_type)), h_type,
+                    checked(&mean, 0, b, at::kFloat), checked(&rstd, 0, b, at::kFloat), checked(gamma, 0, d, scalar(p_type)), p_type,
+                    checked(dH, b, d, scalar(dx_type)), rows(dY), cols(dY), checked(&dX, b, d, scalar(dx_type)), dx_type,
+                    checked(dgamma, 0, d, scalar(p_type)), checked(dbeta, 0, d, scalar(p_type)), ws.at, ws.bytes);
+    });
+}
+SLOPE_PY(slope_linear_bwd_dw_masked_q8) {
+    return guarded(args, n, [](Args& a) {
+        const at::Tensor &dY = a.matrix(), &Xc = a.tensor(), &mask = a.matrix(), &dWc = a.matrix();
+        const Scratch ws(a.tensor_or_none());
+        const int64_t b = dY.size(0), d_out = dY.size(1), d_in = 8 * mask.size(1);
+        return call(p_slope_linear_bwd_dw_masked_q8, checked(&dY, b, d_out, at::kBFloat16), checked_checkpoint(&Xc, b, d_in), rows(dY),
+                    cols(dY), static_cast<int>(d_in), checked(&mask, d_out, d_in / 8, at::kByte), checked(&dWc, d_out, d_in / 2, at::kBFloat16),
+                    ws.at, ws.bytes);
+    });
+}
+SLOPE_PY(slope_linear_bwd_dw_adapter_q8) {
+    return guarded(args, n, [](Args& a) {
+        const at::Tensor &dY = a.matrix(), &Xc = a.tensor(), &T = a.matrix(), &dT = a.matrix(), &mask = a.matrix(), &dWc = a.matrix(),
+                         &dL = a.matrix(), &dR = a.matrix();
+        const Scratch ws(a.tensor_or_none());
+        const int64_t b = dY.size(0), d_out = dY.size(1), d_in = 8 * mask.size(1), r = T.size(1);
+        return call(p_slope_linear_bwd_dw_adapter_q8, checked(&dY, b, d_out, at::kBFloat16), checked_checkpoint(&Xc, b, d_in),
+                    checked(&T, b, r, at::kBFloat16), checked(&dT, b, r, at::kBFloat16), rows(dY), cols(dY), static_cast<int>(d_in), cols(T),
+                    checked(&mask, d_out, d_in / 8, at::kByte), checked(&dWc, d_out, d_in / 2, at::kBFloat16),
+                    checked(&dL, d_in, r, at::kBFloat16), checked(&dR, r, d_out, at::kBFloat16), ws.at, ws.bytes);
+    });
+}
+SLOPE_PY(slope_dense_linear_bwd_dw_q8) {
+    return guarded(args, n, [](Args& a) {
+        const at::Tensor &dY = a.matrix(), &Xc = a.tensor(), &dW = a.matrix();
+        const Scratch ws(a.tensor_or_none());
+        const int64_t b = dY.size(0), d_out = dY.size(1), d_in = dW.size(1);
+        return call(p_slope_dense_linear_bwd_dw_q8, checked(&dY, b, d_out, at::kBFloat16), checked_checkpoint(&Xc, b, d_in), rows(dY), cols(dY),
+                    static_cast<int>(d_in), checked(&dW, d_out, d_in, at::kBFloat16), ws.at, ws.bytes);
     });
 }
 
