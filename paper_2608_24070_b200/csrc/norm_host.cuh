@@ -7,53 +7,81 @@ namespace slope {
 static bool plain_type(int t) { return t == SLOPE_BF16 || t == SLOPE_F32; }
 static bool checkpoint_dims_ok(int rows, int cols) { return rows > 0 && cols > 0 && cols % kQBlock == 0; }
 
-// How the rows of a layer norm are laid over warps: `chunks` times eight columns per lane.
+// How the rows of a layer norm are laid over a block: `chunks` times eight columns per lane, `row_warps` warps per row, `groups` rows at a time.
 struct NormPlan {
-    int row_warps, chunks, groups, blocks;
+    int row_warps, chunks, groups, batch, blocks, shared_bytes;
     int threads() const { return 32 * row_warps * groups; }
 };
-static NormPlan norm_fwd_plan(int b, int d) {
+// Four chunks and few warps per row as far as that goes: what a row costs beside its columns (two sums over its warps, its place in the ring) is
+// shared by more of them.  us, two / three / four chunks: backward 8192 x 5120 from 8 bits 98 / 82 / 76, 16384 x 4096 94 / 123 / 94, forward 8192 x 5120 48 / 42 / 37.
+// `warps`, `per_sm`: of a block, and blocks of an SM.
+static NormPlan norm_plan(int b, int d, int warps, int per_sm, int sms) {
     const int units = (d + 255) / 256;                        // warps that a row fills with one chunk per lane
-    NormPlan p;
-    p.row_warps = (units + 3) / 4;
+    NormPlan p{(units + 3) / 4, 0, 0, 1, 0, 0};
     p.chunks = (units + p.row_warps - 1) / p.row_warps;
-    p.groups = std::max(1, 8 / p.row_warps);
-    p.blocks = (b + p.groups - 1) / p.groups;
+    p.groups = std::max(1, warps / p.row_warps);
+    if (p.row_warps > 1) p.groups = std::min(p.groups, 15);   // (named barriers)
+    // adjacent rows that travel together: up to 2 KB of bf16, as long as every group gets two such batches
+    while (p.batch < 8 && 8 * p.batch * d <= 4096 && 4ll * p.batch * p.groups * sms <= b) p.batch *= 2;
+    p.blocks = std::min((b + p.groups * p.batch - 1) / (p.groups * p.batch), sms * per_sm);
+    p.shared_bytes = per_sm > 1 ? kNormSharedBytes / 2 - 2048 : kNormSharedBytes;
     return p;
+}
+// Two blocks of 12 warps, so that one of them works while the other begins or ends, unless a row takes more than half of one: us, one block of 24 /
+// two of 12: 8192 x 768 with both checkpoints 25.6 / 22.7, 2039 x 5120 14.7 / 13.1; 4096 x 8192 49 / 53.
+static NormPlan norm_fwd_plan(int b, int d, const DeviceInfo& info) {
+    const bool two = d <= 6 * 1024;
+    return norm_plan(b, d, two ? kNormFwdWarps / 2 : kNormFwdWarps, two ? 2 : 1, info.sm_count);
 }
 // (the caller's workspace follows from the blocks and is asked for with no device at hand: the SM count is the B200's)
-static NormPlan norm_bwd_plan(int b, int d) {
-    constexpr int kSms = 148;
-    const int units = (d + 255) / 256;
-    NormPlan p;
-    p.chunks = units > 16 ? 2 : 1;
-    p.row_warps = (units + p.chunks - 1) / p.chunks;
-    p.groups = std::max(1, std::min(kNormMaxGroups, 16 / p.row_warps));
-    const int resident = p.row_warps > 16 ? 1 : 2;
-    p.blocks = std::min((b + p.groups - 1) / p.groups, resident * kSms);
-    return p;
-}
+static NormPlan norm_bwd_plan(int b, int d) { return norm_plan(b, d, kNormBwdWarps, 1, 148); }
 
-template <typename... KArgs, typename... Args>
-static slope_status_t launch_rows(void (*kern)(KArgs...), int blocks, int threads, int smem_bytes, cudaStream_t stream, Args&&... args) {
-    return launch_cluster_ex(kern, blocks, 1, threads, smem_bytes, /*overlap_prologue=*/true, stream, std::forward<Args>(args)...);
+// The ring of a launch, gamma and beta behind it.
+static NormRing norm_ring(const NormPlan& plan, int b, int d, const void* gamma, const void* beta, int params, int p_type, const void* s0, int bytes0,
+                          const void* s1, int bytes1, const void* s2, int bytes2) {
+    NormRing r{{static_cast<const uint8_t*>(s0), static_cast<const uint8_t*>(s1), static_cast<const uint8_t*>(s2)},
+               {bytes0, s1 ? bytes1 : 0, s2 ? bytes2 : 0}, plan.batch, 0, plan.groups, plan.row_warps, b, d, {gamma, beta}, p_type == SLOPE_F32, params};
+    r.stages = std::max(1, std::min(kNormMaxStages, (plan.shared_bytes - r.param_bytes()) / (r.groups * r.stage_bytes())));
+    return r;
+}
+template <typename Params>
+static slope_status_t launch_norm(void (*kern)(const Params), const NormPlan& plan, int least_bytes, cudaStream_t stream, const Params& p) {
+    const int smem = std::max(p.ring.bytes() + p.ring.param_bytes(), least_bytes);
+    if (!set_smem(kern, kNormSharedBytes)) return SLOPE_ERR_CUDA;
+    return launch_cluster_ex(kern, plan.blocks, 1, plan.threads(), smem, /*overlap_prologue=*/true, stream, p);
+}
+template <int TYPE, int CHUNKS>
+static slope_status_t launch_norm_fwd_of(const NormPlan& plan, const NormFwdParams& p, cudaStream_t stream) {
+    const bool full = p.ring.d == 256 * plan.row_warps * CHUNKS, residual = p.ring.src[1], ckpt = p.H_ckpt || p.Y_ckpt;
+    const auto pick = [&](auto r, auto c) {
+        return full ? layer_norm_fwd_kernel<TYPE, CHUNKS, true, r.value, c.value> : layer_norm_fwd_kernel<TYPE, CHUNKS, false, r.value, c.value>;
+    };
+    using Yes = std::true_type;
+    using No = std::false_type;
+    return launch_norm(residual ? (ckpt ? pick(Yes{}, Yes{}) : pick(Yes{}, No{})) : ckpt ? pick(No{}, Yes{}) : pick(No{}, No{}), plan, 0, stream, p);
 }
 template <int TYPE>
 static slope_status_t launch_norm_fwd(const NormPlan& plan, const NormFwdParams& p, cudaStream_t stream) {
-    auto kern = plan.chunks == 1   ? layer_norm_fwd_kernel<TYPE, 1>
-                : plan.chunks == 2 ? layer_norm_fwd_kernel<TYPE, 2>
-                : plan.chunks == 3 ? layer_norm_fwd_kernel<TYPE, 3>
-                                   : layer_norm_fwd_kernel<TYPE, 4>;
-    return launch_rows(kern, plan.blocks, plan.threads(), 0, stream, p);
+    return plan.chunks == 1   ? launch_norm_fwd_of<TYPE, 1>(plan, p, stream)
+           : plan.chunks == 2 ? launch_norm_fwd_of<TYPE, 2>(plan, p, stream)
+           : plan.chunks == 3 ? launch_norm_fwd_of<TYPE, 3>(plan, p, stream)
+                              : launch_norm_fwd_of<TYPE, 4>(plan, p, stream);
+}
+template <int TYPE, int DX_TYPE, int CHUNKS>
+static slope_status_t launch_norm_bwd_of(const NormPlan& plan, const NormBwdParams& p, cudaStream_t stream) {
+    const bool full = p.ring.d == 256 * plan.row_warps * CHUNKS, side = p.ring.src[2];
+    // (the groups' sums of the parameters' gradients take the place of the ring in the end)
+    return launch_norm(full ? (side ? layer_norm_bwd_kernel<TYPE, DX_TYPE, CHUNKS, true, true> : layer_norm_bwd_kernel<TYPE, DX_TYPE, CHUNKS, true, false>)
+                            : side ? layer_norm_bwd_kernel<TYPE, DX_TYPE, CHUNKS, false, true> : layer_norm_bwd_kernel<TYPE, DX_TYPE, CHUNKS, false, false>,
+                       plan, plan.groups * 8 * p.ring.d, stream, p);
 }
 template <int TYPE, int DX_TYPE>
 static slope_status_t launch_norm_bwd(const NormPlan& plan, const NormBwdParams& p, cudaStream_t stream) {
-    auto kern = plan.row_warps > 16 ? layer_norm_bwd_kernel<TYPE, DX_TYPE, 2, 1024>
-                : plan.chunks == 2  ? layer_norm_bwd_kernel<TYPE, DX_TYPE, 2, 512>
-                                    : layer_norm_bwd_kernel<TYPE, DX_TYPE, 1, 512>;
-    return launch_rows(kern, plan.blocks, plan.threads(), plan.groups > 1 ? 8 * p.d : 0, stream, p);
+    return plan.chunks == 1   ? launch_norm_bwd_of<TYPE, DX_TYPE, 1>(plan, p, stream)
+           : plan.chunks == 2 ? launch_norm_bwd_of<TYPE, DX_TYPE, 2>(plan, p, stream)
+           : plan.chunks == 3 ? launch_norm_bwd_of<TYPE, DX_TYPE, 3>(plan, p, stream)
+                              : launch_norm_bwd_of<TYPE, DX_TYPE, 4>(plan, p, stream);
 }
-
 }  // namespace slope
 
 extern "C" {
@@ -71,7 +99,7 @@ slope_status_t slope_checkpoint_store(const void* X, int x_type, int rows, int c
     if (slope_status_t st = check_arch(info)) return st;
     const size_t n8 = static_cast<size_t>(rows) * cols / 8;
     return launch_stream(x_type == SLOPE_F32 ? checkpoint_store_kernel<kTypeF32> : checkpoint_store_kernel<kTypeBf16>,
-                         dim3(stream_grid(n8, info)), static_cast<cudaStream_t>(stream), X, n8, checkpoint);
+                         dim3(stream_grid(n8 / 2 + 1, info)), static_cast<cudaStream_t>(stream), X, n8, checkpoint);
 }
 
 slope_status_t slope_checkpoint_load(const void* checkpoint, int rows, int cols, void* X, int x_type, void* stream) {
@@ -82,7 +110,7 @@ slope_status_t slope_checkpoint_load(const void* checkpoint, int rows, int cols,
     if (slope_status_t st = check_arch(info)) return st;
     const size_t n8 = static_cast<size_t>(rows) * cols / 8;
     return launch_stream(x_type == SLOPE_F32 ? checkpoint_load_kernel<kTypeF32> : checkpoint_load_kernel<kTypeBf16>,
-                         dim3(stream_grid(n8, info)), static_cast<cudaStream_t>(stream), checkpoint, n8, X);
+                         dim3(stream_grid(n8 / 2 + 1, info)), static_cast<cudaStream_t>(stream), checkpoint, n8, X);
 }
 
 slope_status_t slope_layer_norm_fwd(const void* X, int x_type, const void* residual, const void* gamma, const void* beta, int p_type,
@@ -97,9 +125,9 @@ slope_status_t slope_layer_norm_fwd(const void* X, int x_type, const void* resid
         if (!aligned16(p)) return SLOPE_ERR_ALIGNMENT;
     DeviceInfo info;
     if (slope_status_t st = check_arch(info)) return st;
-    const NormPlan plan = norm_fwd_plan(b, d);
-    const NormFwdParams p{X, residual, gamma, beta, H, Y, H_ckpt, Y_ckpt, static_cast<float*>(mean), static_cast<float*>(rstd),
-                          b, d, plan.row_warps, p_type == SLOPE_F32, eps};
+    const NormPlan plan = norm_fwd_plan(b, d, info);
+    const NormFwdParams p{norm_ring(plan, b, d, gamma, beta, 2, p_type, X, x_type == SLOPE_F32 ? 4 * d : 2 * d, residual, 2 * d, nullptr, 0), H, Y, H_ckpt, Y_ckpt,
+                          static_cast<float*>(mean), static_cast<float*>(rstd), eps};
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     return x_type == SLOPE_F32 ? launch_norm_fwd<kTypeF32>(plan, p, stream) : launch_norm_fwd<kTypeBf16>(plan, p, stream);
 }
@@ -125,8 +153,10 @@ slope_status_t slope_layer_norm_bwd(const void* dY, const void* H, int h_type, c
     DeviceInfo info;
     if (slope_status_t st = check_arch(info)) return st;
     const NormPlan plan = norm_bwd_plan(b, d);
-    const NormBwdParams p{dY, H, gamma, dH, static_cast<const float*>(mean), static_cast<const float*>(rstd), dX, dgamma, dbeta,
-                          static_cast<float*>(workspace), b, d, plan.row_warps, p_type == SLOPE_F32};
+    const int h_bytes = h_type == SLOPE_F32 ? 4 * d : h_type == SLOPE_Q8 ? d : 2 * d;
+    const NormBwdParams p{norm_ring(plan, b, d, gamma, nullptr, plan.chunks > 2, p_type, H, h_bytes, dY, 2 * d, dH, dx_type == SLOPE_F32 ? 4 * d : 2 * d),
+                          static_cast<const uint8_t*>(H) + static_cast<size_t>(b) * d, static_cast<const float*>(mean),
+                          static_cast<const float*>(rstd), dX, dgamma, dbeta, static_cast<float*>(workspace)};
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     const bool wide = dx_type == SLOPE_F32;
     slope_status_t st;
@@ -134,7 +164,8 @@ slope_status_t slope_layer_norm_bwd(const void* dY, const void* H, int h_type, c
     else if (h_type == SLOPE_F32) st = wide ? launch_norm_bwd<kTypeF32, kTypeF32>(plan, p, stream) : launch_norm_bwd<kTypeF32, kTypeBf16>(plan, p, stream);
     else st = wide ? launch_norm_bwd<kTypeQ8, kTypeF32>(plan, p, stream) : launch_norm_bwd<kTypeQ8, kTypeBf16>(plan, p, stream);
     if (st != SLOPE_OK || !params || plan.blocks == 1) return st;
-    return launch_rows(layer_norm_params_kernel, (2 * d + 127) / 128, 256, 0, stream, p.partial, plan.blocks, d, dgamma, dbeta, p.p_f32);
+    return launch_cluster_ex(layer_norm_params_kernel, (2 * d + 31) / 32, 1, 256, 0, /*overlap_prologue=*/true, stream, p.partial, plan.blocks, d,
+                             dgamma, dbeta, p.ring.p_f32);
 }
 
 // ------------------------------------------------------------------ weight gradients from a checkpoint
