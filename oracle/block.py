@@ -101,9 +101,22 @@ def causal_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, batch: i
     return out.permute(0, 2, 1, 3).reshape(batch * seq, heads * hd)
 
 
+def layer_norm(x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor, eps: float) -> torch.Tensor:
+    c = x - x.mean(dim=-1, keepdim=True)
+    return c / torch.sqrt((c * c).mean(dim=-1, keepdim=True) + eps) * gamma + beta
+
+
 def decoder_block(x: torch.Tensor, layers: Dict[str, LayerF64], batch: int, seq: int, heads: int, eps: float = 1e-5,
-                  linear=slope_linear) -> torch.Tensor:
-    """x [batch*seq, d] -> block output [batch*seq, d]."""
+                  linear=slope_linear, norms=None) -> torch.Tensor:
+    """x [batch*seq, d] -> block output [batch*seq, d]; ``norms``: (gamma, beta) of the two layer norms that take the place of the
+    RMS normalisation."""
+    if norms is not None:
+        n1 = layer_norm(x, *norms[0], eps)
+        a = causal_attention(linear(n1, layers["q"]), linear(n1, layers["k"]), linear(n1, layers["v"]), batch, seq, heads)
+        h = x + linear(a, layers["o"])
+        n2 = layer_norm(h, *norms[1], eps)
+        g = torch.nn.functional.silu(linear(n2, layers["gate"])) * linear(n2, layers["up"])
+        return h + linear(g, layers["down"])
     n1 = rms_norm(x, eps)
     a = causal_attention(linear(n1, layers["q"]), linear(n1, layers["k"]), linear(n1, layers["v"]), batch, seq, heads)
     h = x + linear(a, layers["o"])
@@ -113,11 +126,11 @@ def decoder_block(x: torch.Tensor, layers: Dict[str, LayerF64], batch: int, seq:
 
 
 def block_fwd_bwd(x_bits: np.ndarray, dout_bits: np.ndarray, layers: Dict[str, LayerF64], batch: int, seq: int,
-                  heads: int, eps: float = 1e-5, linear=slope_linear):
+                  heads: int, eps: float = 1e-5, linear=slope_linear, norms=None):
     """Forward and backward of the block for the loss <out, dOut>.
 
     Returns (out, dx, grads) as float64 numpy arrays; grads[name] = dict(dW=mask1 (.) dY^T X [d_out, d_in],
-    dL, dR).  Clears the gradients held by ``layers`` first.
+    dL, dR).  Clears the gradients held by ``layers`` first.  ``norms``: float64 leaves, which hold their gradients afterwards.
     """
     for lay in layers.values():
         for t in (lay.WR, lay.L, lay.R):
@@ -125,7 +138,7 @@ def block_fwd_bwd(x_bits: np.ndarray, dout_bits: np.ndarray, layers: Dict[str, L
                 t.grad = None
     x = torch.from_numpy(bf16_to_f64(x_bits)).requires_grad_(True)
     dout = torch.from_numpy(bf16_to_f64(dout_bits))
-    out = decoder_block(x, layers, batch, seq, heads, eps, linear)
+    out = decoder_block(x, layers, batch, seq, heads, eps, linear, norms)
     out.backward(dout)
     grads = {}
     for name, lay in layers.items():
