@@ -339,8 +339,9 @@ slope_status_t slope_layer_norm_bwd(const void* dY, const void* H, int h_type, c
 
 /*
  * The weight gradients with X from its checkpoint: the outputs of slope_linear_bwd_dw_masked, slope_linear_bwd_dw_adapter and
- * slope_dense_linear_bwd_dw for the matrix that the checkpoint reads back as (rounded once, sums in an order of their own).
- * `workspace`: device scratch of at least slope_bwd_dw_q8_workspace_bytes() bytes (r = 0: no adapters; NULL if that is 0).
+ * slope_dense_linear_bwd_dw for the matrix that the checkpoint reads back as, bit for bit.
+ * `workspace`: device scratch of at least slope_bwd_dw_q8_workspace_bytes() bytes (r = 0: no adapters); X is read back into it, so that
+ * one workspace serves all layers of a model in turn.
  */
 size_t slope_bwd_dw_q8_workspace_bytes(int b, int d_out, int d_in, int r);
 slope_status_t slope_linear_bwd_dw_masked_q8(const void* dY, const void* X_ckpt, int b, int d_out, int d_in,

@@ -1,6 +1,8 @@
 // Host side of the layer norm, of the 8-bit checkpoints of activations and of the weight gradients from them: part of slope_lib.cu,
 // whose argument checks, plans and launches it uses.
 #pragma once
+#include <cfloat>
+
 #include "norm_kernels.cuh"
 
 namespace slope {
@@ -23,14 +25,14 @@ static NormPlan norm_plan(int b, int d, int warps, int per_sm, int sms) {
     if (p.row_warps > 1) p.groups = std::min(p.groups, 15);   // (named barriers)
     // adjacent rows that travel together: up to 2 KB of bf16, as long as every group gets two such batches
     while (p.batch < 8 && 8 * p.batch * d <= 4096 && 4ll * p.batch * p.groups * sms <= b) p.batch *= 2;
-    p.blocks = std::min((b + p.groups * p.batch - 1) / (p.groups * p.batch), sms * per_sm);
+    p.blocks = std::min((b - 1) / (p.groups * p.batch) + 1, sms * per_sm);
     p.shared_bytes = per_sm > 1 ? kNormSharedBytes / 2 - 2048 : kNormSharedBytes;
     return p;
 }
-// Two blocks of 12 warps, so that one of them works while the other begins or ends, unless a row takes more than half of one: us, one block of 24 /
-// two of 12: 8192 x 768 with both checkpoints 25.6 / 22.7, 2039 x 5120 14.7 / 13.1; 4096 x 8192 49 / 53.
+// Two blocks of 12 warps, so that one of them works while the other begins or ends, as long as two rows each fit beside gamma and beta: us, one
+// block of 24 / two of 12: 8192 x 768 with both checkpoints 25.6 / 22.7, 2039 x 5120 14.7 / 13.1; 4096 x 8192 49 / 53.
 static NormPlan norm_fwd_plan(int b, int d, const DeviceInfo& info) {
-    const bool two = d <= 6 * 1024;
+    const bool two = d <= 5 * 1024;
     return norm_plan(b, d, two ? kNormFwdWarps / 2 : kNormFwdWarps, two ? 2 : 1, info.sm_count);
 }
 // (the caller's workspace follows from the blocks and is asked for with no device at hand: the SM count is the B200's)
@@ -116,7 +118,7 @@ slope_status_t slope_checkpoint_load(const void* checkpoint, int rows, int cols,
 slope_status_t slope_layer_norm_fwd(const void* X, int x_type, const void* residual, const void* gamma, const void* beta, int p_type,
                                     int b, int d, float eps, void* H, void* Y, void* mean, void* rstd, void* H_ckpt, void* Y_ckpt,
                                     void* stream_) {
-    if (!X || !Y || !plain_type(x_type) || !plain_type(p_type) || !(eps >= 0.0f)) return SLOPE_ERR_INVALID_ARG;
+    if (!X || !Y || !plain_type(x_type) || !plain_type(p_type) || !(eps >= 0.0f && eps <= FLT_MAX)) return SLOPE_ERR_INVALID_ARG;
     if ((H && !residual) || !mean != !rstd) return SLOPE_ERR_INVALID_ARG;
     if (b < 1 || d < 1 || d % 8 != 0 || d > kNormMaxWidth) return SLOPE_ERR_SHAPE;
     if ((H_ckpt || Y_ckpt) && !checkpoint_dims_ok(b, d)) return SLOPE_ERR_SHAPE;
@@ -169,6 +171,10 @@ slope_status_t slope_layer_norm_bwd(const void* dY, const void* H, int h_type, c
 }
 
 // ------------------------------------------------------------------ weight gradients from a checkpoint
+// X is read back into the workspace and multiplied by the bf16 kernels: 3.03 bytes of HBM traffic per value in front of a product that the tensor
+// cores bound (16384 tokens 11008 -> 4096: 84 of 1080 us).  Converting inside the product instead, codes by TMA into a ring, eight warps that
+// write the operand tile, gave the same bits at 1256 us: a k-block of 256 x 256 x 64 keeps an SM's shared memory busy for 512 clocks as
+// it is (what TMA brings, what the MMAs read), the time that the MMAs take, and the conversion adds 350.
 size_t slope_bwd_dw_q8_workspace_bytes(int b, int d_out, int d_in, int r) {
     if (b <= 0 || d_out <= 0 || d_in <= 0 || r < 0) return 0;
     return align256(static_cast<size_t>(b) * d_in * 2) + slope_bwd_dw_adapter_workspace_bytes(b, d_out, d_in, r);

@@ -163,6 +163,28 @@ def test_dense_weight_gradient_from_a_checkpoint(B, b, d_out, d_in):
     assert parity_error(f64(dW), f64(t["dY"]).T @ t["X"]) <= REL_TOL
 
 
+@pytest.mark.parametrize("b,d_out,d_in,r", [(1, 128, 128, 0), (300, 512, 640, 16), (1000, 2304, 768, 0), (777, 3200, 3328, 64), (5700, 1792, 2048, 0)])
+def test_the_bits_are_those_of_the_matrix_read_back(B, b, d_out, d_in, r):
+    import torch
+
+    t = layer(B, b, d_out, d_in, r, 5)
+    X = torch.empty(b, d_in, dtype=torch.bfloat16, device="cuda")
+    B.slope_checkpoint_load(t["Xc"], X)
+    want = {k: torch.empty_like(t[k]) for k in ("dWc", "dL", "dR") if k in t}
+    if r:
+        ws = torch.empty(B.slope_bwd_dw_adapter_workspace_bytes(b, d_out, d_in, r), dtype=torch.uint8, device="cuda")
+        B.slope_linear_bwd_dw_adapter(t["dY"], X, t["T"], t["dT"], t["mask"], want["dWc"], want["dL"], want["dR"], ws)
+        B.slope_linear_bwd_dw_adapter_q8(t["dY"], t["Xc"], t["T"], t["dT"], t["mask"], t["dWc"], t["dL"], t["dR"], t["ws"])
+    else:
+        B.slope_linear_bwd_dw_masked(t["dY"], X, t["mask"], want["dWc"])
+        B.slope_linear_bwd_dw_masked_q8(t["dY"], t["Xc"], t["mask"], t["dWc"], t["ws"])
+        dense = [torch.empty(d_out, d_in, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        B.slope_dense_linear_bwd_dw(t["dY"], X, dense[0])
+        B.slope_dense_linear_bwd_dw_q8(t["dY"], t["Xc"], dense[1], t["ws"])
+        assert torch.equal(dense[0], dense[1])
+    assert all(torch.equal(want[k], t[k]) for k in want)
+
+
 @pytest.mark.parametrize("b,d_out,d_in", [(200, 256, 512), (700, 2560, 4096)])
 def test_an_overflow_shows_in_the_gradient(B, b, d_out, d_in):
     """A block that held an infinity reads back as NaN: the columns of its 32 inputs are NaN in every row, no other is."""

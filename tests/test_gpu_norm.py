@@ -124,6 +124,14 @@ def test_forward(B, b, d, x, p):
     assert B.slope_poll_status() == 0
 
 
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+@pytest.mark.parametrize("b,d", [(3, 16384), (5, 5632), (7, 6144), (20011, 64), (15001, 200), (30011, 8), (9999, 512)])
+def test_forward_at_the_edges_of_its_plans(B, b, d, x):
+    """The widest rows with all that a block has to hold, and rows so short and many that several travel together."""
+    c = case(b, d, x, "f32", b + d, residual=True)
+    check_forward(B, c, forward(B, c, 1e-5), 1e-5, x)
+
+
 def test_forward_at_inference_is_the_same(B):
     """Without statistics, sum and checkpoints: the same Y, bit for bit."""
     import torch
@@ -213,6 +221,17 @@ def test_backward(B, b, d, x, dx, p):
     got = backward(B, c, out, out["Hc"] if x == "q8" else c["X"], dx, p, dh)
     check_backward(c, out, h, got, dx, p, dh)
     assert B.slope_poll_status() == 0
+
+
+@pytest.mark.parametrize("x", ["bf16", "f32", "q8"])
+@pytest.mark.parametrize("b,d", [(20011, 64), (30011, 32), (9999, 512)])
+def test_backward_of_many_short_rows(B, b, d, x):
+    kind = "bf16" if x == "q8" else x
+    c = case(b, d, kind, "f32", b, offset=0.1)
+    out = forward(B, c, 1e-5, ckpt=x == "q8")
+    h = ref.decode(*ref.split(out["Hc"].cpu().numpy(), b, d)) if x == "q8" else f64(c["X"])
+    got = backward(B, c, out, out["Hc"] if x == "q8" else c["X"], kind, "f32")
+    check_backward(c, out, h, got, kind, "f32")
 
 
 def test_gradients_against_differences(B):

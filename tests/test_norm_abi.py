@@ -54,7 +54,7 @@ def test_layer_norm_refusals(lib, a):
         return lib.slope_layer_norm_fwd(X, x_type, residual, gamma, beta, p_type, b, d, eps, H, Y, mean, rstd, Hc, Yc, None)
 
     assert fwd(X=None) == 1 and fwd(Y=None) == 1 and fwd(x_type=Q8) == 1 and fwd(p_type=Q8) == 1
-    assert fwd(eps=-1.0) == 1 and fwd(eps=float("nan")) == 1
+    assert fwd(eps=-1.0) == 1 and fwd(eps=float("nan")) == 1 and fwd(eps=float("inf")) == 1
     assert fwd(H=a) == 1                                                           # a sum without a residual
     assert fwd(mean=a) == 1 and fwd(rstd=a) == 1                                   # one statistic without the other
     assert fwd(b=0) == 2 and fwd(d=0) == 2 and fwd(d=12) == 2 and fwd(d=16392) == 2
