@@ -29,11 +29,12 @@ static NormPlan norm_plan(int b, int d, int warps, int per_sm, int sms) {
     p.shared_bytes = per_sm > 1 ? kNormSharedBytes / 2 - 2048 : kNormSharedBytes;
     return p;
 }
-// Two blocks of 12 warps, so that one of them works while the other begins or ends, as long as two rows each fit beside gamma and beta: us, one
-// block of 24 / two of 12: 8192 x 768 with both checkpoints 25.6 / 22.7, 2039 x 5120 14.7 / 13.1; 4096 x 8192 49 / 53.
+// Two blocks of 12 warps, so that one of them works while the other begins or ends, as long as two rows each fit beside gamma and beta, else one
+// of 16: us, one block of 24 / two of 12: 8192 x 768 with both checkpoints 25.6 / 22.2, 2039 x 5120 14.7 / 13.1; 4096 x 8192 49 / 53, with
+// 24 / 16 warps 49 / 50, with a checkpoint of Y 74.7 / 70.5.
 static NormPlan norm_fwd_plan(int b, int d, const DeviceInfo& info) {
     const bool two = d <= 5 * 1024;
-    return norm_plan(b, d, two ? kNormFwdWarps / 2 : kNormFwdWarps, two ? 2 : 1, info.sm_count);
+    return norm_plan(b, d, two ? kNormFwdWarps / 2 : 16, two ? 2 : 1, info.sm_count);
 }
 // (the caller's workspace follows from the blocks and is asked for with no device at hand: the SM count is the B200's)
 static NormPlan norm_bwd_plan(int b, int d) { return norm_plan(b, d, kNormBwdWarps, 1, 148); }

@@ -26,8 +26,7 @@ constexpr int kTypeBf16 = 0, kTypeF32 = 1, kTypeQ8 = 2;          // == slope_typ
 constexpr int kQBlock = 32;
 
 // ---------------------------------------------------------------- eight values of a row, as fp32
-// In four pairs, for the instructions that work on two fp32 values at once: what these kernels issue, not what they add and multiply, is
-// what HBM has to wait for (see layer_norm_fwd_kernel).
+// In four pairs, for the instructions that work on two fp32 values at once: what these kernels issue is what HBM has to wait for (see below).
 using Pair = unsigned long long;
 struct V8 {
     Pair p[4];
@@ -173,7 +172,7 @@ __device__ __forceinline__ void store_q8(void* ckpt, size_t at, size_t count, bo
 
 // ---------------------------------------------------------------- matrices to checkpoints and back
 // A thread takes eight values at a time, two times in one go so that twice the bytes are in flight; `n8` eights in all, a multiple of 4, so that a
-// block's four lanes live or rest together.  16384 x 11008 to 8 bits and back 197 us with one at a time.
+// block's four lanes live or rest together.  HBM-bound: 16384 x 11008 to 8 bits and back 1093 MB in 182 us, 6.0 TB/s (one at a time: 197 us).
 template <int TYPE>
 __global__ void __launch_bounds__(256) checkpoint_store_kernel(const void* X, size_t n8, void* ckpt) {
     griddep_stream(8);
@@ -210,11 +209,16 @@ __global__ void __launch_bounds__(256) checkpoint_load_kernel(const void* ckpt, 
 }
 
 // ---------------------------------------------------------------- layer norm
-// A block is as large as an SM holds, and stays.  A row belongs to a group of `row_warps` warps; a lane holds CHUNKS times eight of its columns,
-// chunk i of lane l at column 8 (l + 32 row_warps i), the same ones in all rows, so that gamma, beta and their gradients stay in
-// registers.  Rows come in by bulk copies, ahead of their use, into the group's ring in shared memory: the bytes in flight that HBM needs (some 35 KB
+// Blocks fill the SMs and stay.  A row belongs to a group of `row_warps` warps; a lane holds CHUNKS times eight of its columns, chunk i of lane l at
+// column 8 (l + 32 row_warps i), the same ones in all rows, so that the sums of gamma's and beta's gradients can stay in registers.
+// Rows come in by bulk copies, ahead of their use, into the group's ring in shared memory: the bytes in flight that HBM needs (some 35 KB
 // per SM) cost no registers.  A stage holds `batch` adjacent rows (several where they are short), one copy per matrix; the group's first lane
 // asks for the next ones when the group has read it.  Groups have nothing to do with one another.
+//
+// What bounds them: HBM for long rows (16384 x 4096: forward 6.0, backward 5.6 of 6.45 TB/s), else what is issued and waited for per row: at HBM's
+// rate an SM has 890 clocks for a row of 5120 values.  us of the forward of 8192 x 5120 with fp32 parameters, 168 MB (floor 26), as it went: rows loaded by
+// the warps, one fp32 value per instruction 62; the same from the ring, instances without branches on what a call leaves out, two values per
+// instruction (23.6 -> 11.6 instructions per value) 43; 24 warps instead of 16 37; loads that leave L2 first 35.
 constexpr int kNormMaxWidth = 16384;
 constexpr int kNormFwdWarps = 24, kNormBwdWarps = 16;             // of a block at most: so many as leave a row its registers
 constexpr int kNormWarps = kNormFwdWarps;
@@ -391,6 +395,7 @@ struct NormRows {
         return (t.x + t.y) + (t.z + t.w);
     }
 };
+
 struct NormFwdParams {
     NormRing ring;                // X, residual
     void *H, *Y, *H_ckpt, *Y_ckpt;
@@ -504,7 +509,11 @@ __device__ __forceinline__ void store_param(void* base, bool f32, int at, float 
 }
 
 // gamma's and beta's gradients grow in registers; at the end the groups' sums meet in shared memory (where the ring was) and are added in
-// order, and the blocks' sums are added in order by layer_norm_params_kernel (a single block writes the gradients itself).
+// order, and the blocks' sums are added in order by layer_norm_params_kernel (a single block writes the gradients itself).  The order depends on
+// the sizes alone.
+// Registers are what it is short of: four chunks' sums take 64, so that from three chunks on a row's values are not kept between its two sums and its
+// output but read from the ring and normalised again.  us, one / two (kept) / four (read again) chunks per lane: 16384 x 4096 140 / 94 / 94, 8192 x 5120 from
+// 8 bits 76 / 98 / 76, 4096 x 8192 56 / 58 / 56, 8192 x 768 from 8 bits 18.9 / 21 / 18.9 (three chunks).
 template <int TYPE, int DX_TYPE, int CHUNKS, bool FULL, bool SIDE>
 __global__ void __launch_bounds__(32 * kNormBwdWarps, 1) layer_norm_bwd_kernel(const __grid_constant__ NormBwdParams p) {
     constexpr bool kReread = CHUNKS > 2;      // a row does not fit in registers beside its columns' sums: it is read from the ring twice
