@@ -29,21 +29,23 @@ static NormPlan norm_plan(int b, int d, int warps, int per_sm, int sms) {
     p.shared_bytes = per_sm > 1 ? kNormSharedBytes / 2 - 2048 : kNormSharedBytes;
     return p;
 }
-// Two blocks of 12 warps, so that one of them works while the other begins or ends, as long as two rows each fit beside gamma and beta, else one
-// of 16: us, one block of 24 / two of 12: 8192 x 768 with both checkpoints 25.6 / 22.2, 2039 x 5120 14.7 / 13.1; 4096 x 8192 49 / 53, with
-// 24 / 16 warps 49 / 50, with a checkpoint of Y 74.7 / 70.5.
-static NormPlan norm_fwd_plan(int b, int d, const DeviceInfo& info) {
-    const bool two = d <= 5 * 1024;
+// Two blocks of 12 warps, so that one of them works while the other begins or ends, or one of 16, whose ring has two stages where those of two blocks
+// have one: for rows of which two do not fit in half the memory beside gamma and beta, and, with checkpoints, from 4096 on.  us, one block of 24 / two of 12:
+// 8192 x 768 with both checkpoints 25.6 / 22.2, 2039 x 5120 14.7 / 13.1, 4096 x 8192 49 / 53; one of 16 / two of 12: 4096 x 8192 50 / 53, with a
+// checkpoint of Y 16384 x 4096 140 / 144, 8192 x 5120 90.5 / 92.5, 4096 x 3584 34.9 / 34.2, 8192 x 768 18.8 / 16.8.
+static NormPlan norm_fwd_plan(int b, int d, bool ckpt, const DeviceInfo& info) {
+    const bool two = ckpt ? d < 4096 : d <= 5 * 1024;
     return norm_plan(b, d, two ? kNormFwdWarps / 2 : 16, two ? 2 : 1, info.sm_count);
 }
 // (the caller's workspace follows from the blocks and is asked for with no device at hand: the SM count is the B200's)
 static NormPlan norm_bwd_plan(int b, int d) { return norm_plan(b, d, kNormBwdWarps, 1, 148); }
 
-// The ring of a launch, gamma and beta behind it.
-static NormRing norm_ring(const NormPlan& plan, int b, int d, const void* gamma, const void* beta, int params, int p_type, const void* s0, int bytes0,
+// The ring of a launch, gamma and beta behind it.  `leave_first`: us, rows leave L2 first / like others: forward 16384 x 4096 90 / 95, in fp32 139 / 147; but
+// with a checkpoint of Y (written and then read back) 140 / 136, in fp32 189 / 181.
+static NormRing norm_ring(const NormPlan& plan, int b, int d, bool leave_first, const void* gamma, const void* beta, int params, int p_type, const void* s0, int bytes0,
                           const void* s1, int bytes1, const void* s2, int bytes2) {
     NormRing r{{static_cast<const uint8_t*>(s0), static_cast<const uint8_t*>(s1), static_cast<const uint8_t*>(s2)},
-               {bytes0, s1 ? bytes1 : 0, s2 ? bytes2 : 0}, plan.batch, 0, plan.groups, plan.row_warps, b, d, {gamma, beta}, p_type == SLOPE_F32, params};
+               {bytes0, s1 ? bytes1 : 0, s2 ? bytes2 : 0}, plan.batch, 0, plan.groups, plan.row_warps, b, d, leave_first, {gamma, beta}, p_type == SLOPE_F32, params};
     r.stages = std::max(1, std::min(kNormMaxStages, (plan.shared_bytes - r.param_bytes()) / (r.groups * r.stage_bytes())));
     return r;
 }
@@ -128,8 +130,8 @@ slope_status_t slope_layer_norm_fwd(const void* X, int x_type, const void* resid
         if (!aligned16(p)) return SLOPE_ERR_ALIGNMENT;
     DeviceInfo info;
     if (slope_status_t st = check_arch(info)) return st;
-    const NormPlan plan = norm_fwd_plan(b, d, info);
-    const NormFwdParams p{norm_ring(plan, b, d, gamma, beta, 2, p_type, X, x_type == SLOPE_F32 ? 4 * d : 2 * d, residual, 2 * d, nullptr, 0), H, Y, H_ckpt, Y_ckpt,
+    const NormPlan plan = norm_fwd_plan(b, d, H_ckpt || Y_ckpt, info);
+    const NormFwdParams p{norm_ring(plan, b, d, !H_ckpt && !Y_ckpt, gamma, beta, 2, p_type, X, x_type == SLOPE_F32 ? 4 * d : 2 * d, residual, 2 * d, nullptr, 0), H, Y, H_ckpt, Y_ckpt,
                           static_cast<float*>(mean), static_cast<float*>(rstd), eps};
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     return x_type == SLOPE_F32 ? launch_norm_fwd<kTypeF32>(plan, p, stream) : launch_norm_fwd<kTypeBf16>(plan, p, stream);
@@ -157,7 +159,7 @@ slope_status_t slope_layer_norm_bwd(const void* dY, const void* H, int h_type, c
     if (slope_status_t st = check_arch(info)) return st;
     const NormPlan plan = norm_bwd_plan(b, d);
     const int h_bytes = h_type == SLOPE_F32 ? 4 * d : h_type == SLOPE_Q8 ? d : 2 * d;
-    const NormBwdParams p{norm_ring(plan, b, d, gamma, nullptr, plan.chunks > 2, p_type, H, h_bytes, dY, 2 * d, dH, dx_type == SLOPE_F32 ? 4 * d : 2 * d),
+    const NormBwdParams p{norm_ring(plan, b, d, true, gamma, nullptr, plan.chunks > 2, p_type, H, h_bytes, dY, 2 * d, dH, dx_type == SLOPE_F32 ? 4 * d : 2 * d),
                           static_cast<const uint8_t*>(H) + static_cast<size_t>(b) * d, static_cast<const float*>(mean),
                           static_cast<const float*>(rstd), dX, dgamma, dbeta, static_cast<float*>(workspace)};
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);

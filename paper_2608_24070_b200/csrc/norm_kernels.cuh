@@ -229,6 +229,7 @@ struct NormRing {
     const uint8_t* src[kNormMaxSources];      // row-major matrices; nullptr: none
     int row_bytes[kNormMaxSources];           // multiples of 16
     int batch, stages, groups, row_warps, b, d;
+    int leave_first;                          // rows that have been read leave L2 before others
     const void* param[2];                     // gamma, beta (nullptr: ones, zeros)
     int p_f32;
     int params;                               // how many of them are kept in shared memory
@@ -237,6 +238,11 @@ struct NormRing {
     __host__ __device__ int bytes() const { return groups * stages * stage_bytes(); }
 };
 
+__device__ __forceinline__ uint64_t l2_policy_evict_normal() {
+    uint64_t pol;
+    asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(pol));
+    return pol;
+}
 __device__ __forceinline__ void bulk_load(uint32_t smem_dst, const void* src, uint32_t bytes, uint64_t* bar, uint64_t policy) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;"
                  ::"r"(smem_dst), "l"(src), "r"(bytes), "r"(smem_u32(bar)), "l"(policy)
@@ -328,7 +334,7 @@ struct NormRows {
         if (first >= static_cast<uint32_t>(r.b)) return;
         const uint32_t rows = min(static_cast<uint32_t>(r.batch), r.b - first);
         uint64_t* bar = &sh.full[group][s];
-        const uint64_t policy = l2_policy_evict_first();          // (read once)
+        const uint64_t policy = r.leave_first ? l2_policy_evict_first() : l2_policy_evict_normal();
         mbar_expect_tx(bar, rows * (r.row_bytes[0] + r.row_bytes[1] + r.row_bytes[2]));
         uint32_t to = data + s * r.stage_bytes();
 #pragma unroll
