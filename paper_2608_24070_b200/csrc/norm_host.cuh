@@ -37,8 +37,14 @@ static NormPlan norm_fwd_plan(int b, int d, bool ckpt, const DeviceInfo& info) {
     const bool two = ckpt ? d < 4096 : d <= 5 * 1024;
     return norm_plan(b, d, two ? kNormFwdWarps / 2 : 16, two ? 2 : 1, info.sm_count);
 }
-// (the caller's workspace follows from the blocks and is asked for with no device at hand: the SM count is the B200's)
-static NormPlan norm_bwd_plan(int b, int d) { return norm_plan(b, d, kNormBwdWarps, 1, 148); }
+// One block of 16 warps per SM, or two of 8 where a row is one warp's: they begin and end apart.  Not for up to 16 rows, which one block takes without a second launch, nor
+// for many rows of at most 512.  us, one / two: 256 x 512 6.3 / 5.5, 2048 x 512 7.3 / 7.6, 8192 x 512 13.4 / 14.9,
+// 100 x 768 7.5 / 6.3, 2048 x 768 8.6 / 8.9, 16384 x 768 27.6 / 25.8, 32768 x 1024 55.3 / 54.8, 16 x 512 4.6 / 5.2.
+// (The caller's workspace follows from the blocks and is asked for with no device at hand: the SM count is the B200's.)
+static NormPlan norm_bwd_plan(int b, int d) {
+    const bool two = d <= 1024 && b > kNormBwdWarps && (d > 512 || b <= 1024);
+    return norm_plan(b, d, two ? kNormBwdWarps / 2 : kNormBwdWarps, two ? 2 : 1, 148);
+}
 
 // The ring of a launch, gamma and beta behind it.  `leave_first`: us, rows leave L2 first / like others: forward 16384 x 4096 90 / 95, in fp32 139 / 147; but
 // with a checkpoint of Y (written and then read back) 140 / 136, in fp32 189 / 181.

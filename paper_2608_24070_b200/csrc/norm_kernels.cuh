@@ -5,8 +5,7 @@
 //   backward   x = (h - m) s,  g = dY gamma,  dX = s (g - mean(g) - x mean(g x)) (+ dH),
 //              dgamma = sum over the tokens of dY x,  dbeta = sum over the tokens of dY
 //
-// Everything here is bound by HBM: every matrix is read once and written once, and a row stays in registers
-// between its statistics and its output.  All sums are fp32; the variance is that of the differences from the mean, not
+// Every matrix is read once from HBM and written once; a row stays in registers or shared memory between its statistics and its output.  All sums are fp32; the variance is that of the differences from the mean, not
 // mean(h^2) - m^2, which cancels where a row's mean is large beside its spread.
 //
 // Checkpoint of a matrix [rows x cols], cols a multiple of 32: each block of 32 consecutive values of a row is 32 signed bytes
