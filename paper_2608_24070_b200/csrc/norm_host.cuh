@@ -16,10 +16,10 @@ struct NormPlan {
 };
 // Four chunks and few warps per row as far as that goes: what a row costs beside its columns (two sums over its warps, its place in the ring) is
 // shared by more of them.  us, two / three / four chunks: backward 8192 x 5120 from 8 bits 98 / 82 / 76, 16384 x 4096 94 / 123 / 94, forward 8192 x 5120 48 / 42 / 37.
-// `warps`, `per_sm`: of a block, and blocks of an SM.
-static NormPlan norm_plan(int b, int d, int warps, int per_sm, int sms) {
+// `most`, `warps`, `per_sm`: chunks of a lane, warps of a block and blocks of an SM.
+static NormPlan norm_plan(int b, int d, int most, int warps, int per_sm, int sms) {
     const int units = (d + 255) / 256;                        // warps that a row fills with one chunk per lane
-    NormPlan p{(units + 3) / 4, 0, 0, 1, 0, 0};
+    NormPlan p{(units + most - 1) / most, 0, 0, 1, 0, 0};
     p.chunks = (units + p.row_warps - 1) / p.row_warps;
     p.groups = std::max(1, warps / p.row_warps);
     if (p.row_warps > 1) p.groups = std::min(p.groups, 15);   // (named barriers)
@@ -33,9 +33,16 @@ static NormPlan norm_plan(int b, int d, int warps, int per_sm, int sms) {
 // have one: for rows of which two do not fit in half the memory beside gamma and beta, and, with checkpoints, from 4096 on.  us, one block of 24 / two of 12:
 // 8192 x 768 with both checkpoints 25.6 / 22.2, 2039 x 5120 14.7 / 13.1, 4096 x 8192 49 / 53; one of 16 / two of 12: 4096 x 8192 50 / 53, with a
 // checkpoint of Y 16384 x 4096 140 / 144, 8192 x 5120 90.5 / 92.5, 4096 x 3584 34.9 / 34.2, 8192 x 768 18.8 / 16.8.
-static NormPlan norm_fwd_plan(int b, int d, bool ckpt, const DeviceInfo& info) {
+// An fp32 stream with a residual and without checkpoints moves 12 bytes per value and has little else to do: two chunks a lane, so that fewer rows are under
+// way at a time (two per SM at 4096), and rows that leave L2 like others.  us, as above / so: 8192 x 3584 63.8 / 57.8, 16384 x 4096 139 / 127 (98 % of a copy),
+// 8192 x 5120 91.5 / 83, 8192 x 6144 110 / 103, 8192 x 8192 139.5 / 127, 8192 x 2304 41.6 / 39.4, but 16384 x 2048 70 / 72.6; bf16 16384 x 4096 90 / 92, 8192 x 5120 59 / 82.
+static bool norm_fwd_heavy(int d, int x_type, bool residual, bool ckpt) {
+    return x_type == SLOPE_F32 && residual && !ckpt && d > 2048 && d <= 8192;
+}
+static NormPlan norm_fwd_plan(int b, int d, bool heavy, bool ckpt, const DeviceInfo& info) {
+    if (heavy) return norm_plan(b, d, 2, d <= 4096 ? 16 : kNormFwdWarps, 1, info.sm_count);
     const bool two = ckpt ? d < 4096 : d <= 5 * 1024;
-    return norm_plan(b, d, two ? kNormFwdWarps / 2 : 16, two ? 2 : 1, info.sm_count);
+    return norm_plan(b, d, 4, two ? kNormFwdWarps / 2 : 16, two ? 2 : 1, info.sm_count);
 }
 // One block of 16 warps per SM, or two of 8 where a row is one warp's: they begin and end apart.  Not for up to 16 rows, which one block takes without a second launch, nor
 // for many rows of at most 512.  us, one / two: 256 x 512 6.3 / 5.5, 2048 x 512 7.3 / 7.6, 8192 x 512 13.4 / 14.9,
@@ -43,7 +50,7 @@ static NormPlan norm_fwd_plan(int b, int d, bool ckpt, const DeviceInfo& info) {
 // (The caller's workspace follows from the blocks and is asked for with no device at hand: the SM count is the B200's.)
 static NormPlan norm_bwd_plan(int b, int d) {
     const bool two = d <= 1024 && b > kNormBwdWarps && (d > 512 || b <= 1024);
-    return norm_plan(b, d, two ? kNormBwdWarps / 2 : kNormBwdWarps, two ? 2 : 1, 148);
+    return norm_plan(b, d, 4, two ? kNormBwdWarps / 2 : kNormBwdWarps, two ? 2 : 1, 148);
 }
 
 // The ring of a launch, gamma and beta behind it.  `leave_first`: us, rows leave L2 first / like others: forward 16384 x 4096 90 / 95, in fp32 139 / 147; but
@@ -136,8 +143,9 @@ slope_status_t slope_layer_norm_fwd(const void* X, int x_type, const void* resid
         if (!aligned16(p)) return SLOPE_ERR_ALIGNMENT;
     DeviceInfo info;
     if (slope_status_t st = check_arch(info)) return st;
-    const NormPlan plan = norm_fwd_plan(b, d, H_ckpt || Y_ckpt, info);
-    const NormFwdParams p{norm_ring(plan, b, d, !H_ckpt && !Y_ckpt, gamma, beta, 2, p_type, X, x_type == SLOPE_F32 ? 4 * d : 2 * d, residual, 2 * d, nullptr, 0), H, Y, H_ckpt, Y_ckpt,
+    const bool ckpt = H_ckpt || Y_ckpt, heavy = norm_fwd_heavy(d, x_type, residual, ckpt);
+    const NormPlan plan = norm_fwd_plan(b, d, heavy, ckpt, info);
+    const NormFwdParams p{norm_ring(plan, b, d, !ckpt && !heavy, gamma, beta, 2, p_type, X, x_type == SLOPE_F32 ? 4 * d : 2 * d, residual, 2 * d, nullptr, 0), H, Y, H_ckpt, Y_ckpt,
                           static_cast<float*>(mean), static_cast<float*>(rstd), eps};
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     return x_type == SLOPE_F32 ? launch_norm_fwd<kTypeF32>(plan, p, stream) : launch_norm_fwd<kTypeBf16>(plan, p, stream);
