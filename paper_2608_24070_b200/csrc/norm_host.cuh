@@ -39,8 +39,12 @@ static NormPlan norm_plan(int b, int d, int most, int warps, int per_sm, int sms
 static bool norm_fwd_heavy(int d, int x_type, bool residual, bool ckpt) {
     return x_type == SLOPE_F32 && residual && !ckpt && d > 2048 && d <= 8192;
 }
+// Wider than 8192: three chunks on up to 24 warps, two rows at a time up to 9216 (what a block's memory holds of an fp32 row with its residual, gamma and beta).
+// 4096 rows, us, four chunks on 16 warps / so: 8448 bf16 55 / 31, with residual and checkpoint 104 / 75, in fp32 114 / 97; 11008 57 / 55, 113 / 107, 133 / 128; 13824
+// 65 / 56.5, 130 / 116, 165 / 162; 16384 62 / 70, 142 / 143, 192 / 188.
 static NormPlan norm_fwd_plan(int b, int d, bool heavy, bool ckpt, const DeviceInfo& info) {
     if (heavy) return norm_plan(b, d, 2, d <= 4096 ? 16 : kNormFwdWarps, 1, info.sm_count);
+    if (d > 8192 && d <= 15 * 1024) return norm_plan(b, d, 3, kNormFwdWarps, 1, info.sm_count);
     const bool two = ckpt ? d < 4096 : d <= 5 * 1024;
     return norm_plan(b, d, 4, two ? kNormFwdWarps / 2 : 16, two ? 2 : 1, info.sm_count);
 }

@@ -125,7 +125,7 @@ def test_forward(B, b, d, x, p):
 
 
 @pytest.mark.parametrize("x", ["bf16", "f32"])
-@pytest.mark.parametrize("b,d", [(3, 16384), (5, 5632), (7, 6144), (6, 2312), (301, 4096), (150, 4608), (40, 8192), (20011, 64), (15001, 200), (30011, 8), (9999, 512)])
+@pytest.mark.parametrize("b,d", [(3, 16384), (5, 9216), (4, 9224), (3, 11008), (3, 15360), (2, 15368), (5, 5632), (7, 6144), (6, 2312), (301, 4096), (150, 4608), (40, 8192), (20011, 64), (15001, 200), (30011, 8), (9999, 512)])
 def test_forward_at_the_edges_of_its_plans(B, b, d, x):
     """The widest rows with all that a block has to hold, and rows so short and many that several travel together."""
     c = case(b, d, x, "f32", b + d, residual=True)
