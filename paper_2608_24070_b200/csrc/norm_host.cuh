@@ -32,7 +32,8 @@ static NormPlan norm_plan(int b, int d, int most, int warps, int per_sm, int sms
 // Two blocks of 12 warps, so that one of them works while the other begins or ends, or one of 16, whose ring has two stages where those of two blocks
 // have one: for rows of which two do not fit in half the memory beside gamma and beta, and, with checkpoints, from 4096 on.  us, one block of 24 / two of 12:
 // 8192 x 768 with both checkpoints 25.6 / 22.2, 2039 x 5120 14.7 / 13.1, 4096 x 8192 49 / 53; one of 16 / two of 12: 4096 x 8192 50 / 53, with a
-// checkpoint of Y 16384 x 4096 140 / 144, 8192 x 5120 90.5 / 92.5, 4096 x 3584 34.9 / 34.2, 8192 x 768 18.8 / 16.8.
+// checkpoint of Y 16384 x 4096 140 / 144, 8192 x 5120 90.5 / 92.5, 4096 x 3584 34.9 / 34.2, 8192 x 768 18.8 / 16.8.  Up to 6144 one block of 24, which has four rows at a time
+// and not two: 4096 x 6144 with a checkpoint 61 / 42; 4096 x 8192 with residual and checkpoint 70 / 75.
 // An fp32 stream with a residual and without checkpoints moves 12 bytes per value and has little else to do: two chunks a lane, so that fewer rows are under
 // way at a time (two per SM at 4096), and rows that leave L2 like others.  us, as above / so: 8192 x 3584 63.8 / 57.8, 16384 x 4096 139 / 127 (98 % of a copy),
 // 8192 x 5120 91.5 / 83, 8192 x 6144 110 / 103, 8192 x 8192 139.5 / 127, 8192 x 2304 41.6 / 39.4, but 16384 x 2048 70 / 72.6; bf16 16384 x 4096 90 / 92, 8192 x 5120 59 / 82.
@@ -46,15 +47,19 @@ static NormPlan norm_fwd_plan(int b, int d, bool heavy, bool ckpt, const DeviceI
     if (heavy) return norm_plan(b, d, 2, d <= 4096 ? 16 : kNormFwdWarps, 1, info.sm_count);
     if (d > 8192 && d <= 15 * 1024) return norm_plan(b, d, 3, kNormFwdWarps, 1, info.sm_count);
     const bool two = ckpt ? d < 4096 : d <= 5 * 1024;
-    return norm_plan(b, d, 4, two ? kNormFwdWarps / 2 : 16, two ? 2 : 1, info.sm_count);
+    return norm_plan(b, d, 4, two ? kNormFwdWarps / 2 : d > 5120 && d <= 6144 ? kNormFwdWarps : 16, two ? 2 : 1, info.sm_count);
 }
 // One block of 16 warps per SM, or two of 8 where a row is one warp's: they begin and end apart.  Not for up to 16 rows, which one block takes without a second launch, nor
 // for many rows of at most 512.  us, one / two: 256 x 512 6.3 / 5.5, 2048 x 512 7.3 / 7.6, 8192 x 512 13.4 / 14.9,
 // 100 x 768 7.5 / 6.3, 2048 x 768 8.6 / 8.9, 16384 x 768 27.6 / 25.8, 32768 x 1024 55.3 / 54.8, 16 x 512 4.6 / 5.2.
+// Three chunks where four would have no more rows at a time: us, four / three, 4096 rows from 8 bits: 5376 48 / 44.5, 6144 55 / 48, 8448 83 / 70, 11008 90 / 86,
+// 12288 104 / 91; bf16 8448 75 / 65, 11008 82 / 83; fp32 12288 184 / 160.
 // (The caller's workspace follows from the blocks and is asked for with no device at hand: the SM count is the B200's.)
 static NormPlan norm_bwd_plan(int b, int d) {
     const bool two = d <= 1024 && b > kNormBwdWarps && (d > 512 || b <= 1024);
-    return norm_plan(b, d, 4, two ? kNormBwdWarps / 2 : kNormBwdWarps, two ? 2 : 1, 148);
+    const int units = (d + 255) / 256, w3 = (units + 2) / 3, w4 = (units + 3) / 4;
+    const int most = w3 <= kNormBwdWarps && kNormBwdWarps / w3 == kNormBwdWarps / w4 ? 3 : 4;
+    return norm_plan(b, d, most, two ? kNormBwdWarps / 2 : kNormBwdWarps, two ? 2 : 1, 148);
 }
 
 // The ring of a launch, gamma and beta behind it.  `leave_first`: us, rows leave L2 first / like others: forward 16384 x 4096 90 / 95, in fp32 139 / 147; but

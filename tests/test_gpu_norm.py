@@ -224,8 +224,8 @@ def test_backward(B, b, d, x, dx, p):
 
 
 @pytest.mark.parametrize("x", ["bf16", "f32", "q8"])
-@pytest.mark.parametrize("b,d", [(20011, 64), (30011, 32), (9999, 512)])
-def test_backward_of_many_short_rows(B, b, d, x):
+@pytest.mark.parametrize("b,d", [(20011, 64), (30011, 32), (9999, 512), (17, 768), (1025, 512), (330, 5376), (7, 6144), (301, 9216), (2, 12288), (150, 4608)])
+def test_backward_at_the_edges_of_its_plans(B, b, d, x):
     kind = "bf16" if x == "q8" else x
     c = case(b, d, kind, "f32", b, offset=0.1)
     out = forward(B, c, 1e-5, ckpt=x == "q8")
