@@ -13,6 +13,8 @@ one's output and its gradient by the next one's.  ``DenseLinear`` is the same bl
 With ``norms`` the block has the layer norms of GPT-2, OPT and BERT instead, on the library's calls, residual adds
 included (``LayerNorm``).  ``checkpoint=True`` of a layer keeps what its backward pass needs of its input in 8 bits: the layer norm of the
 stream, the linears of their inputs; linears that share an input share its checkpoint, which the layer norm in front of them writes.
+Their calls' workspaces (a decoded matrix of activations among them) are allocated for the one call and go back to torch's caching allocator behind it, so that
+all layers of a model use the same memory in turn and nothing stays; what a captured graph needs comes from that graph's own pool.
 
 Every linear call is bracketed by CUDA events when ``timers`` is given, so the time spent in
 the linears can be summed separately from the torch glue.
@@ -62,7 +64,7 @@ class SlopeLinear:
         self.dL = None if L is None else torch.empty_like(L)
         self.dR = None if R is None else torch.empty_like(R)
         self.workspace = None
-        if self.r and max_tokens:
+        if self.r and max_tokens and not checkpoint:
             n = B.slope_adapter_workspace_bytes(max_tokens, self.d_out, self.d_in, self.r)
             self.workspace = torch.empty(max(n, 16), dtype=torch.uint8, device=W.device)
         self.checkpoint = checkpoint
@@ -72,10 +74,9 @@ class SlopeLinear:
         """``kept``: a checkpoint of X that is there already (``checkpoint`` layers; else they store one)."""
         return _SlopeLinearFn.apply(X, self, kept)
 
-    def scratch(self, nbytes: int, device) -> torch.Tensor:
-        if self.workspace is None or self.workspace.numel() < nbytes:
-            self.workspace = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device)
-        return self.workspace
+
+def _scratch(nbytes: int, device) -> torch.Tensor:
+    return torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device)
 
 
 class _SlopeLinearFn(torch.autograd.Function):
@@ -120,13 +121,15 @@ class _SlopeLinearFn(torch.autograd.Function):
                 if layer.checkpoint:
                     B.slope_adapter_fwd_bwd(2, None, dY, None, layer.R, *sizes, dT=dT)
                 else:
-                    workspace = layer.scratch(B.slope_adapter_workspace_bytes(*sizes), dY.device)
-                    B.slope_adapter_fwd_bwd(1, X, dY, layer.L, layer.R, *sizes, T=T, dT=dT, dL=layer.dL, dR=layer.dR, workspace=workspace)
+                    need = B.slope_adapter_workspace_bytes(*sizes)
+                    if layer.workspace is None or layer.workspace.numel() < need:
+                        layer.workspace = _scratch(need, dY.device)
+                    B.slope_adapter_fwd_bwd(1, X, dY, layer.L, layer.R, *sizes, T=T, dT=dT, dL=layer.dL, dR=layer.dR, workspace=layer.workspace)
             B.slope_linear_bwd_dx(dY, layer.WTc_vals, layer.WTc_meta, layer.d_in, dX, dT, layer.L)
             if not layer.checkpoint:
                 B.slope_linear_bwd_dw_masked(dY, X, layer.mask1, layer.dWc)
                 return
-            workspace = layer.scratch(B.slope_bwd_dw_q8_workspace_bytes(*sizes), dY.device)
+            workspace = _scratch(B.slope_bwd_dw_q8_workspace_bytes(*sizes), dY.device)
             if layer.r:
                 B.slope_linear_bwd_dw_adapter_q8(dY, X, T, dT, layer.mask1, layer.dWc, layer.dL, layer.dR, workspace)
             else:
@@ -144,7 +147,6 @@ class LayerNorm:
     def __init__(self, gamma: torch.Tensor, beta: torch.Tensor, eps: float = 1e-5, checkpoint: bool = False):
         self.gamma, self.beta, self.eps, self.checkpoint = gamma, beta, eps, checkpoint
         self.dgamma, self.dbeta = torch.empty_like(gamma), torch.empty_like(beta)
-        self.workspace: Optional[torch.Tensor] = None
 
     def __call__(self, X: torch.Tensor, residual: Optional[torch.Tensor] = None):
         """(stream, output, checkpoint of the output or None): the stream is X, or X + residual."""
@@ -180,10 +182,8 @@ class _LayerNormFn(torch.autograd.Function):
         dY = dY.contiguous()
         b, d = dY.shape
         dX = torch.empty(b, d, dtype=ctx.dtype, device=dY.device)
-        need = B.slope_layer_norm_bwd_workspace_bytes(b, d)
-        if norm.workspace is None or norm.workspace.numel() < need:
-            norm.workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=dY.device)
-        B.slope_layer_norm_bwd(dY, H, mean, rstd, norm.gamma, dX, norm.dgamma, norm.dbeta, norm.workspace, None if dH is None else dH.contiguous())
+        workspace = _scratch(B.slope_layer_norm_bwd_workspace_bytes(b, d), dY.device)
+        B.slope_layer_norm_bwd(dY, H, mean, rstd, norm.gamma, dX, norm.dgamma, norm.dbeta, workspace, None if dH is None else dH.contiguous())
         # (the residual is a sub-layer's bf16 output, whatever the stream's type)
         return dX, dX.to(torch.bfloat16) if ctx.with_residual else None, None
 
