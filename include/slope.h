@@ -316,7 +316,9 @@ slope_status_t slope_checkpoint_load(const void* checkpoint, int rows, int cols,
  *   mean, rstd  for the backward pass; both NULL at inference
  *   H_ckpt      checkpoint of h (of X without a residual), for slope_layer_norm_bwd, or NULL     } d a multiple of 32
  *   Y_ckpt      checkpoint of Y, for the weight gradients of the layers behind it, or NULL        }
- * Otherwise outputs must not overlap inputs or one another.  A row with an infinity or a NaN has NaN statistics and outputs.
+ * Otherwise outputs must not overlap inputs or one another.  The rows may be of any magnitude, sums and squares beyond fp32 among them.  A row
+ * with an infinity or a NaN has a mean that is infinite or NaN, and NaN in rstd and throughout Y; so have rstd and Y of a row in which some h - m is none of
+ * fp32's numbers.
  */
 slope_status_t slope_layer_norm_fwd(const void* X, int x_type, const void* residual, const void* gamma, const void* beta, int p_type,
                                     int b, int d, float eps, void* H, void* Y, void* mean, void* rstd,

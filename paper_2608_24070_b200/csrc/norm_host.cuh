@@ -1,8 +1,6 @@
 // Host side of the layer norm, of the 8-bit checkpoints of activations and of the weight gradients from them: part of slope_lib.cu,
 // whose argument checks, plans and launches it uses.
 #pragma once
-#include <cfloat>
-
 #include "norm_kernels.cuh"
 
 namespace slope {
