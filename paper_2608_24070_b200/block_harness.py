@@ -25,6 +25,7 @@ from typing import Dict, List, Optional, Tuple
 
 import torch
 import torch.nn.functional as F
+from torch.autograd.function import once_differentiable
 
 from . import binding as B
 
@@ -105,6 +106,7 @@ class _SlopeLinearFn(torch.autograd.Function):
         return Y
 
     @staticmethod
+    @once_differentiable                 # (linear in dY: with a dY that is a constant there is nothing to refuse)
     def backward(ctx, dY):
         layer: SlopeLinear = ctx.layer
         saved = ctx.saved_tensors
@@ -137,6 +139,22 @@ class _SlopeLinearFn(torch.autograd.Function):
 
         _timed(layer.timers, run)
         return dX, None, None
+
+
+class _FirstDerivativeFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, gradient):
+        return gradient.view_as(gradient)
+
+    @staticmethod
+    def backward(ctx, _):
+        raise RuntimeError("LayerNorm has no second derivative")
+
+
+def _first_derivative(gradient: torch.Tensor) -> torch.Tensor:
+    """A gradient that depends on inputs as well as on the gradient that came in: where a graph of the backward pass is asked for, going back
+    through it is an error, instead of a derivative that lacks this part."""
+    return _FirstDerivativeFn.apply(gradient.requires_grad_(True)) if torch.is_grad_enabled() else gradient
 
 
 class LayerNorm:
@@ -184,6 +202,7 @@ class _LayerNormFn(torch.autograd.Function):
         dX = torch.empty(b, d, dtype=ctx.dtype, device=dY.device)
         workspace = _scratch(B.slope_layer_norm_bwd_workspace_bytes(b, d), dY.device)
         B.slope_layer_norm_bwd(dY, H, mean, rstd, norm.gamma, dX, norm.dgamma, norm.dbeta, workspace, None if dH is None else dH.contiguous())
+        dX = _first_derivative(dX)
         # (the residual is a sub-layer's bf16 output, whatever the stream's type)
         return dX, dX.to(torch.bfloat16) if ctx.with_residual else None, None
 
