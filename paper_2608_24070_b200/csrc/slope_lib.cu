@@ -33,6 +33,9 @@ static DeviceInfo device_info() {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return DeviceInfo{};
     if (!cache[dev].ok) {
+        // Makes the device's context this thread's: tensor maps are encoded by the driver itself, which does not do so, and refuses
+        // where the call is the first that the thread makes.
+        if (cudaSetDevice(dev) != cudaSuccess) return DeviceInfo{};
         cudaDeviceProp prop;
         if (cudaGetDeviceProperties(&prop, dev) != cudaSuccess) return DeviceInfo{};
         cache[dev] = DeviceInfo{true, dev, prop.multiProcessorCount, prop.major};
