@@ -295,8 +295,10 @@ slope_status_t slope_adapter_dl_noalloc(const void* X, const void* dT, int b, in
  * of bf16.  (The paper counts weights, gradients and optimizer states only; activations stay dense.)  Of a matrix
  * [rows x cols], cols a multiple of 32, each block of 32 consecutive values of a row is stored as 32 signed bytes times one power
  * of two 2^k: k the smallest integer for which the block's largest magnitude is at most 127.5 * 2^k, within
- * [-126, 121]; code = x / 2^k rounded half to even and held in [-127, 127].  A value that is read back is code * 2^k: off by at
- * most 2^k / 2 (below 2^-126: absolutely), and exact in bf16.  A block with an infinity or a NaN reads back as NaN.
+ * [-126, 121]; code = x / 2^k rounded half to even and held in [-127, 127].  A value that is read back is code * 2^k, exact in bf16, and off by at
+ * most 2^k / 2: at most 1 / 127 of the block's largest magnitude, but for the two ends of k's range.  At k = -126 the error is 2^-127 at most, whatever
+ * the block's size; fp32 values beyond 127.5 * 2^121 (the largest bf16 number) are read back as 127 * 2^121, off by up to 2^121.  A block with an
+ * infinity or a NaN reads back as NaN.
  * Buffer: the rows * cols codes, row-major, then rows * cols / 32 bytes k + 127 (255 for a block of NaN).
  *   slope_checkpoint_store   checkpoint of X (x_type SLOPE_BF16 or SLOPE_F32)
  *   slope_checkpoint_load    X (bf16 or fp32) from a checkpoint

@@ -11,8 +11,9 @@
 //
 // Checkpoint of a matrix [rows x cols], cols a multiple of 32: each block of 32 consecutive values of a row is 32 signed bytes
 // times one power of two, 2^k, k the smallest integer for which the block's largest magnitude is at most 127.5 * 2^k, within
-// [-126, 121]; codes are rounded half to even and held in [-127, 127].  A value is off by at most half a unit of 2^k, i.e.
-// 1/127 of the block's largest magnitude at most (a power of two wastes at most half of the code's range; e4m3 codes, with the
+// [-126, 121]; codes are rounded half to even and held in [-127, 127].  A value is off by at most half a unit of 2^k, i.e. 1/127
+// of the block's largest magnitude at most, but for the ends of k's range: 2^-127 in any block at k = -126, and up to a whole unit for an fp32
+// value beyond 127.5 * 2^121 (a power of two wastes at most half of the code's range; e4m3 codes, with the
 // same 8 bits, are off by up to 1/16 of a value, for Gaussian activations 2.4 % (root mean square) against 0.8 %).  A code has seven
 // significant bits, so a value that is read back is exact in bf16, and a product with it has exactly that operand.
 // Memory: rows * cols codes, then rows * cols / 32 bytes k + 127 (the exponent field of 2^k as fp32); 255, with codes of 0, in a block
