@@ -117,3 +117,37 @@ def test_an_eps_that_outweighs_the_variance(B, d):  # noqa: F811
     out = forward(B, c, float(eps))
     _, mean, rstd, _ = ref.layer_norm(f64(c["X"]), 1.0, 0.0, eps)
     within(f64(out["rstd"]), rstd, rstd * (U * (ADDS + 8) / 2 + 4 * U + (U * ADDS * np.abs(f64(c["X"])).mean(-1) * rstd) ** 2) + 2.0 ** -150, "rstd")
+
+
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [256, 4096])
+def test_such_rows_wherever_the_sum_stands(B, d, x):  # noqa: F811
+    """The sum kept apart, over X, over the residual (bf16), or not at all; and in a graph that is replayed on other rows."""
+    import torch
+
+    c = wide(17, d, x, "f32", d, True)
+    want = forward(B, c, 1e-5)
+    lean = forward(B, c, 1e-5, stats=False, keep_h=False)
+    assert torch.equal(lean["Y"], want["Y"])
+    for place in ("X", "residual") if x == "bf16" else ("X",):
+        X, R, Y = c["X"].clone(), c["residual"].clone(), torch.empty_like(want["Y"])
+        H = X if place == "X" else R
+        B.slope_layer_norm_fwd(X, c["gamma"], c["beta"], 1e-5, Y, residual=R, H=H)
+        assert torch.equal(H, want["H"]) and torch.equal(Y, want["Y"])
+    e = case(17, d, x, "f32", d + 1, True)
+    plain = forward(B, e, 1e-5)
+    X, R, Y, graph = e["X"].clone(), e["residual"].clone(), torch.empty_like(want["Y"]), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.slope_layer_norm_fwd(X, c["gamma"], c["beta"], 1e-5, Y, residual=R)
+    graph.replay()
+    ordinary = Y.clone()
+    X.copy_(c["X"])
+    R.copy_(c["residual"])
+    graph.replay()
+    assert torch.equal(Y, want["Y"])
+    X.copy_(e["X"])
+    R.copy_(e["residual"])
+    graph.replay()
+    assert torch.equal(Y, ordinary)
+    B.slope_layer_norm_fwd(e["X"], e["gamma"], e["beta"], 1e-5, Y, residual=e["residual"])
+    assert torch.equal(Y, plain["Y"])
