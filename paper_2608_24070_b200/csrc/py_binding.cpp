@@ -99,8 +99,16 @@ struct Args {
     }
 };
 
-int rows(const at::Tensor& t) { return static_cast<int>(t.size(0)); }
-int cols(const at::Tensor& t) { return static_cast<int>(t.size(1)); }
+// The C ABI counts rows and columns in int.
+int extent(int64_t n) {
+    if (n != static_cast<int>(n)) {
+        PyErr_SetString(PyExc_OverflowError, "tensor with more than 2^31 - 1 rows or columns");
+        throw Bad{};
+    }
+    return static_cast<int>(n);
+}
+int rows(const at::Tensor& t) { return extent(t.size(0)); }
+int cols(const at::Tensor& t) { return extent(t.size(1)); }
 void* stream() { return c10::cuda::getCurrentCUDAStream().stream(); }
 
 // Runs `body(args)`; C++ exceptions become Python ones.
@@ -370,7 +378,7 @@ SLOPE_PY(slope_linear_bwd_dw_masked_q8) {
         const Scratch ws(a.tensor_or_none());
         const int64_t b = dY.size(0), d_out = dY.size(1), d_in = 8 * mask.size(1);
         return call(p_slope_linear_bwd_dw_masked_q8, checked(&dY, b, d_out, at::kBFloat16), checked_checkpoint(&Xc, b, d_in), rows(dY),
-                    cols(dY), static_cast<int>(d_in), checked(&mask, d_out, d_in / 8, at::kByte), checked(&dWc, d_out, d_in / 2, at::kBFloat16),
+                    cols(dY), extent(d_in), checked(&mask, d_out, d_in / 8, at::kByte), checked(&dWc, d_out, d_in / 2, at::kBFloat16),
                     ws.at, ws.bytes);
     });
 }
@@ -381,7 +389,7 @@ SLOPE_PY(slope_linear_bwd_dw_adapter_q8) {
         const Scratch ws(a.tensor_or_none());
         const int64_t b = dY.size(0), d_out = dY.size(1), d_in = 8 * mask.size(1), r = T.size(1);
         return call(p_slope_linear_bwd_dw_adapter_q8, checked(&dY, b, d_out, at::kBFloat16), checked_checkpoint(&Xc, b, d_in),
-                    checked(&T, b, r, at::kBFloat16), checked(&dT, b, r, at::kBFloat16), rows(dY), cols(dY), static_cast<int>(d_in), cols(T),
+                    checked(&T, b, r, at::kBFloat16), checked(&dT, b, r, at::kBFloat16), rows(dY), cols(dY), extent(d_in), cols(T),
                     checked(&mask, d_out, d_in / 8, at::kByte), checked(&dWc, d_out, d_in / 2, at::kBFloat16),
                     checked(&dL, d_in, r, at::kBFloat16), checked(&dR, r, d_out, at::kBFloat16), ws.at, ws.bytes);
     });
@@ -392,7 +400,7 @@ SLOPE_PY(slope_dense_linear_bwd_dw_q8) {
         const Scratch ws(a.tensor_or_none());
         const int64_t b = dY.size(0), d_out = dY.size(1), d_in = dW.size(1);
         return call(p_slope_dense_linear_bwd_dw_q8, checked(&dY, b, d_out, at::kBFloat16), checked_checkpoint(&Xc, b, d_in), rows(dY), cols(dY),
-                    static_cast<int>(d_in), checked(&dW, d_out, d_in, at::kBFloat16), ws.at, ws.bytes);
+                    extent(d_in), checked(&dW, d_out, d_in, at::kBFloat16), ws.at, ws.bytes);
     });
 }
 
