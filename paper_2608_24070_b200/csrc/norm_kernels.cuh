@@ -389,13 +389,13 @@ struct NormRows {
     // the sum over the group's lanes; of several sums in flight each has a `slot` of its own
     __device__ __forceinline__ void begin_sum(float& v, int slot) const {
         v = warp_sum(v);
-        if (r.row_warps > 1 && (lane & 31) == 0) sh.part[slot][group * padded() + (lane >> 5)] = v;
+        if (r.row_warps > 1 && (lane & 31) == 0) sh.part[slot][group * padded(r.row_warps) + (lane >> 5)] = v;
     }
-    __device__ __forceinline__ int padded() const { return (r.row_warps + 3) & ~3; }
+    static __device__ __forceinline__ int padded(int row_warps) { return (row_warps + 3) & ~3; }
     // (a sync() lies between the two)
     __device__ __forceinline__ float end_sum(float v, int slot) const {
         if (r.row_warps == 1) return v;
-        const float4* part = reinterpret_cast<const float4*>(sh.part[slot] + group * padded());
+        const float4* part = reinterpret_cast<const float4*>(sh.part[slot] + group * padded(r.row_warps));
         float4 t = part[0];
         for (int w = 4; w < r.row_warps; w += 4) {
             const float4 u = part[w >> 2];
@@ -418,14 +418,16 @@ struct NormFwdParams {
     float eps;
 };
 
-// The rows of a group among which some left fp32: their sum, or the sum of their squared differences.  They stand there with an rstd of 0 or NaN and are
-// done once more from the beginning: the mean in units of 2^16 (d / 2^16 of the largest number at most), the variance in units of 2^144, of which d
-// differences of at most 2^128 have d 2^112.  A difference that is itself none of fp32's, or an infinity or a NaN in the row, leaves rstd and Y NaN.
-// Which rows: those whose magnitudes add up to 2^126, or their squared differences, so that none that the kernel's own order of additions took
-// out of range is missed.  h comes from H or, where none is kept, from the inputs (H may be one of them); every thread writes what it has written before.
-// Behind the loop over the rows, out of line and without arguments that the loop would have to keep, so that other rows pay one minimum.  us, without / so /
-// called within the loop / inlined behind it: 8192 x 5120 34.9 / 34.8 / 36.2 / 38.4, 8192 x 2304 16.7 / 16.6 / 17.6 / 17.7, 4096 x 8448 31.4 / 31.4 / 33.1 / 32.8,
-// 4096 x 16384 with residual 105 / 98 / 99 / 99, 16384 x 4096 in fp32 with residual 128 / 130 / 126 / 135.
+// The rows of a group among which some left fp32: their sum, or the sum of their squared differences.  They stand there with an rstd of 0
+// or NaN and are done once more from the beginning: the mean in units of 2^16 (d / 2^16 of the largest number at most), the variance
+// in units of 2^144, of which d differences of at most 2^128 have d 2^112.  A difference that is itself none of fp32's, or an infinity
+// or a NaN in the row, leaves rstd and Y NaN.  Which rows: those that the loop left so, found by its own sums once more, so that a
+// row's bits do not depend on its neighbours.  h comes from H or, where none is kept, from the inputs (H may be one of them); every
+// thread writes what it has written before.
+// Behind the loop over the rows, out of line and without arguments that the loop would have to keep, so that other rows pay one minimum.
+// us, without / so / called within the loop / inlined behind it: 8192 x 5120 34.9 / 34.8 / 36.2 / 38.4, 8192 x 2304
+// 16.7 / 16.6 / 17.6 / 17.7, 4096 x 8448 31.4 / 31.4 / 33.1 / 32.8, 4096 x 16384 with residual 105 / 98 / 99 / 99, 16384 x 4096 in
+// fp32 with residual 128 / 130 / 126 / 135.
 template <int TYPE, bool RESIDUAL, bool CKPT>
 __device__ __noinline__ void layer_norm_wide_rows(const NormFwdParams& p, NormShared& sh, const uint8_t* smem) {
     const int d = p.ring.d, warps = p.ring.row_warps, threads = 32 * warps, group = threadIdx.x / threads, lane = threadIdx.x - group * threads;
@@ -442,44 +444,52 @@ __device__ __noinline__ void layer_norm_wide_rows(const NormFwdParams& p, NormSh
         for (int k = 0; k < 4; ++k) h.p[k] = add2(h.p[k], r.p[k]);
         return TYPE == kTypeBf16 ? from_bf16(to_bf16(h)) : h;
     };
-    const auto group_sum = [&](Pair part, int slot) {
-        const float v = warp_sum(low(part) + high(part));
+    const auto group_sum = [&](const Pair (&part)[2], int slot) {
+        const Pair both_parts = add2(part[0], part[1]);
+        const float v = warp_sum(low(both_parts) + high(both_parts));
         if (warps == 1) return v;
-        const int at = group * ((warps + 3) & ~3);
-        if ((lane & 31) == 0) sh.part[slot][at + (lane >> 5)] = v;
+        float* place = sh.part[slot] + group * NormRows::padded(warps);
+        if ((lane & 31) == 0) place[lane >> 5] = v;
         asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(threads) : "memory");
-        float sum = 0.0f;
-        for (int w = 0; w < warps; ++w) sum += sh.part[slot][at + w];
-        return sum;
+        const float4* sums = reinterpret_cast<const float4*>(place);              // (as NormRows::end_sum adds them)
+        float4 t = sums[0];
+        for (int w = 4; w < warps; w += 4) {
+            const float4 u = sums[w >> 2];
+            t = make_float4(t.x + u.x, t.y + u.y, t.z + u.z, t.w + u.w);
+        }
+        return (t.x + t.y) + (t.z + t.w);
+    };
+    // The row's sum and that of its squared differences, in units and with the loop's order of additions
+    const auto sum_of = [&](float unit, int slot) {
+        Pair part[2] = {0, 0};
+        for (int col = 8 * lane; col < d; col += 8 * threads) {
+            const V8 h = stream(col);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) part[k & 1] = fma2(h.p[k], both(unit), part[k & 1]);
+        }
+        return group_sum(part, slot);
+    };
+    const auto squares_of = [&](float mean, float unit, int slot) {
+        Pair part[2] = {0, 0};
+        for (int col = 8 * lane; col < d; col += 8 * threads) {
+            const V8 h = stream(col);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const Pair v = mul2(add2(h.p[k], both(-mean)), both(unit));
+                part[k & 1] = fma2(v, v, part[k & 1]);
+            }
+        }
+        return group_sum(part, slot);
     };
     // (batches of adjacent rows, as NormRows goes through them)
     const uint32_t b = p.ring.b, batch = p.ring.batch, step = gridDim.x * p.ring.groups * batch;
     for (uint32_t first = (blockIdx.x * p.ring.groups + group) * batch; first < b; first += step) {
         for (uint32_t row = first; row < min(first + batch, b); ++row) {
             base = static_cast<size_t>(row) * d;
-            Pair part = 0, all = 0;
-            for (int col = 8 * lane; col < d; col += 8 * threads) {
-                const V8 h = stream(col);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    part = fma2(h.p[k], both(0x1p-16f), part);
-                    all = fma2(h.p[k] & 0x7FFFFFFF7FFFFFFFull, both(0x1p-16f), all);
-                }
-            }
-            const float mean = group_sum(part, 0) * per * 0x1p16f, magnitude = group_sum(all, 1);
+            if (squares_of(sum_of(1.0f, 0) * per, 1.0f, 1) * per + p.eps <= FLT_MAX) continue;
+            const float mean = sum_of(0x1p-16f, 2) * per * 0x1p16f;
+            const float var = squares_of(mean, 0x1p-72f, 3) * per + p.eps * 0x1p-72f * 0x1p-72f;
             const Pair less = both(-mean);
-            part = 0;
-            for (int col = 8 * lane; col < d; col += 8 * threads) {
-                const V8 h = stream(col);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const Pair v = mul2(add2(h.p[k], less), both(0x1p-72f));
-                    part = fma2(v, v, part);
-                }
-            }
-            const float squares = group_sum(part, 2);
-            if (magnitude < 0x1p110f && squares < 0x1p-18f && p.eps < 0x1p126f) continue;
-            const float var = squares * per + p.eps * 0x1p-72f * 0x1p-72f;
             const float rstd = var <= FLT_MAX ? rsqrtf(var) * 0x1p-72f : __uint_as_float(0x7FC00000u);
             if (p.mean && lane == 0) {
                 p.mean[row] = mean;

@@ -151,3 +151,29 @@ def test_such_rows_wherever_the_sum_stands(B, d, x):  # noqa: F811
     assert torch.equal(Y, ordinary)
     B.slope_layer_norm_fwd(e["X"], e["gamma"], e["beta"], 1e-5, Y, residual=e["residual"])
     assert torch.equal(Y, plain["Y"])
+
+
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [256, 768, 1000, 4096, 8192, 16384])
+def test_rows_next_to_the_range_do_not_depend_on_others(B, d, x):  # noqa: F811
+    """Rows whose squares add up to nearly 2^128, or whose magnitudes do, alone and among rows beyond: the same bits."""
+    import torch
+
+    b = 600
+    gen = torch.Generator().manual_seed(d)
+    rows = torch.randn(6, d, generator=gen, dtype=torch.float64).clamp(-4, 4)
+    near = [rows[k] * (2.0 ** 64 * f / float(rows[k].norm())) for k, f in enumerate((0.99, 0.7, 0.5, 0.36))]
+    near += [rows[4] * (2.0 ** 128 * 0.9 / d / 4) + 2.0 ** 128 * 0.7 / d, rows[5]]          # its sum is in range, its squares are not
+    c = case(b, d, x, "f32", d)
+    for i in range(b):
+        c["X"][i] = near[i % 6].to(c["X"].dtype).cuda()
+    alone = forward(B, c, 1e-5)
+    mixed = dict(c, X=c["X"].clone())
+    beyond = torch.arange(b, device="cuda") % 7 == 3
+    mixed["X"][beyond] = (torch.randn(d, generator=gen, dtype=torch.float64).clamp(-4, 4) * 1e30).to(c["X"].dtype).cuda()
+    out = forward(B, mixed, 1e-5)
+    for k in ("Y", "mean", "rstd"):
+        assert torch.equal(out[k][~beyond], alone[k][~beyond]), k
+        for first in range(6):                       # equal rows of one call, wherever they stand
+            assert (alone[k][first::6] == alone[k][first]).all(), k
+    assert torch.isfinite(out["Y"]).all() and (out["rstd"] > 0).all()
