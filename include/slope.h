@@ -296,9 +296,9 @@ slope_status_t slope_adapter_dl_noalloc(const void* X, const void* dT, int b, in
  * [rows x cols], cols a multiple of 32, each block of 32 consecutive values of a row is stored as 32 signed bytes times one power
  * of two 2^k: k the smallest integer for which the block's largest magnitude is at most 127.5 * 2^k, within
  * [-126, 121]; code = x / 2^k rounded half to even and held in [-127, 127].  A value that is read back is code * 2^k, exact in bf16, and off by at
- * most 2^k / 2: at most 1 / 127 of the block's largest magnitude, but for the two ends of k's range.  At k = -126 the error is 2^-127 at most, whatever
- * the block's size; fp32 values beyond 127.5 * 2^121 (the largest bf16 number) are read back as 127 * 2^121, off by up to 2^121.  A block with an
- * infinity or a NaN reads back as NaN.
+ * most 2^k / 2: at most 1 / 127 of the block's largest magnitude, but for the two ends of k's range.  At k = -126 the error is 2^-127 at
+ * most, whatever the block's size; fp32 values beyond 127.5 * 2^121 (the largest bf16 number) are read back as 127 * 2^121, off by up
+ * to 2^121.  A block with an infinity or a NaN reads back as NaN.
  * Buffer: the rows * cols codes, row-major, then rows * cols / 32 bytes k + 127 (255 for a block of NaN).
  *   slope_checkpoint_store   checkpoint of X (x_type SLOPE_BF16 or SLOPE_F32)
  *   slope_checkpoint_load    X (bf16 or fp32) from a checkpoint
@@ -318,9 +318,10 @@ slope_status_t slope_checkpoint_load(const void* checkpoint, int rows, int cols,
  *   mean, rstd  for the backward pass; both NULL at inference
  *   H_ckpt      checkpoint of h (of X without a residual), for slope_layer_norm_bwd, or NULL     } d a multiple of 32
  *   Y_ckpt      checkpoint of Y, for the weight gradients of the layers behind it, or NULL        }
- * Otherwise outputs must not overlap inputs or one another.  The rows may be of any magnitude, sums and squares beyond fp32 among them.  A row
- * with an infinity or a NaN has a mean that is infinite or NaN, and NaN in rstd and throughout Y; so have rstd and Y of a row in which some h - m is none of
- * fp32's numbers.
+ * Otherwise outputs must not overlap inputs or one another.  The rows may be of any magnitude, sums and squares beyond fp32 among them
+ * (such a row, and one that is not finite, takes its group of warps a second pass over its rows).  A row with an infinity or a NaN has a
+ * mean that is infinite or NaN, and NaN in rstd and throughout Y; rstd and Y are NaN, too, in a row in which some h - m is none of fp32's
+ * numbers.
  */
 slope_status_t slope_layer_norm_fwd(const void* X, int x_type, const void* residual, const void* gamma, const void* beta, int p_type,
                                     int b, int d, float eps, void* H, void* Y, void* mean, void* rstd,
@@ -330,10 +331,10 @@ slope_status_t slope_layer_norm_fwd(const void* X, int x_type, const void* resid
  * Its backward pass: with x = (h - m) s and g = dY gamma,
  *   dX = s (g - mean(g) - x mean(g x)) (+ dH),   dgamma = sum over the rows of dY x,   dbeta = sum over the rows of dY.
  * H is the normalised stream: bf16, fp32 or its checkpoint (h_type SLOPE_Q8; the statistics are still those of the stream itself).
- * dY bf16; dX and dH (the gradient that reaches h past the layer norm, or NULL) of dx_type (bf16 or fp32); dgamma, dbeta [d] of p_type, each NULL if not
- * wanted.  dX may be dH or, where dx_type is bf16, dY; otherwise outputs must not overlap inputs or one another.  The sums over the rows have a
- * fixed order.  `workspace`: device scratch of at least slope_layer_norm_bwd_workspace_bytes() bytes (NULL if that is 0, or if neither dgamma nor
- * dbeta is wanted).
+ * dY bf16; dX and dH (the gradient that reaches h past the layer norm, or NULL) of dx_type (bf16 or fp32); dgamma, dbeta [d] of p_type,
+ * each NULL if not wanted.  dX may be dH or, where dx_type is bf16, dY; otherwise outputs must not overlap inputs or one another.  The
+ * sums over the rows have a fixed order.  `workspace`: device scratch of at least slope_layer_norm_bwd_workspace_bytes() bytes (NULL if
+ * that is 0, or if neither dgamma nor dbeta is wanted).
  */
 size_t slope_layer_norm_bwd_workspace_bytes(int b, int d);
 slope_status_t slope_layer_norm_bwd(const void* dY, const void* H, int h_type, const void* mean, const void* rstd,

@@ -13,8 +13,9 @@ one's output and its gradient by the next one's.  ``DenseLinear`` is the same bl
 With ``norms`` the block has the layer norms of GPT-2, OPT and BERT instead, on the library's calls, residual adds
 included (``LayerNorm``).  ``checkpoint=True`` of a layer keeps what its backward pass needs of its input in 8 bits: the layer norm of the
 stream, the linears of their inputs; linears that share an input share its checkpoint, which the layer norm in front of them writes.
-Their calls' workspaces (a decoded matrix of activations among them) are allocated for the one call and go back to torch's caching allocator behind it, so that
-all layers of a model use the same memory in turn and nothing stays; what a captured graph needs comes from that graph's own pool.
+Their calls' workspaces (a decoded matrix of activations among them) are allocated for the one call and go back to torch's caching
+allocator behind it, so that all layers of a model use the same memory in turn and nothing stays; what a captured graph needs comes from
+that graph's own pool.
 
 Every linear call is bracketed by CUDA events when ``timers`` is given, so the time spent in
 the linears can be summed separately from the torch glue.

@@ -12,8 +12,9 @@ struct NormPlan {
     int row_warps, chunks, groups, batch, blocks, shared_bytes;
     int threads() const { return 32 * row_warps * groups; }
 };
-// Four chunks and few warps per row as far as that goes: what a row costs beside its columns (two sums over its warps, its place in the ring) is
-// shared by more of them.  us, two / three / four chunks: backward 8192 x 5120 from 8 bits 98 / 82 / 76, 16384 x 4096 94 / 123 / 94, forward 8192 x 5120 48 / 42 / 37.
+// Four chunks and few warps per row as far as that goes: what a row costs beside its columns (two sums over its warps, its place in the
+// ring) is shared by more of them.  us, two / three / four chunks: backward 8192 x 5120 from 8 bits 98 / 82 / 76, 16384 x 4096 94 / 123 /
+// 94, forward 8192 x 5120 48 / 42 / 37.
 // `most`, `warps`, `per_sm`: chunks of a lane, warps of a block and blocks of an SM.
 static NormPlan norm_plan(int b, int d, int most, int warps, int per_sm, int sms) {
     const int units = (d + 255) / 256;                        // warps that a row fills with one chunk per lane
@@ -21,38 +22,41 @@ static NormPlan norm_plan(int b, int d, int most, int warps, int per_sm, int sms
     p.chunks = (units + p.row_warps - 1) / p.row_warps;
     p.groups = std::max(1, warps / p.row_warps);
     if (p.row_warps > 1) p.groups = std::min(p.groups, 15);   // (named barriers)
-    // adjacent rows that travel together: up to 2 KB of bf16, as long as every group of the GPU gets two such batches.  us, where that is one batch for the groups of
-    // two blocks per SM / so: 10000 x 512 11.5 / 9.8, 16384 x 256 10.3 / 9.7, 20000 x 128 10.1 / 8.7, 40000 x 64 16.7 / 13.6, but 14000 x 128 6.5 / 7.3; 4 % less on average.
+    // adjacent rows that travel together: up to 2 KB of bf16, as long as every group of the GPU gets two such batches.  us, where that is
+    // one batch for the groups of two blocks per SM / so: 10000 x 512 11.5 / 9.8, 16384 x 256 10.3 / 9.7, 20000 x 128 10.1 / 8.7, 40000 x
+    // 64 16.7 / 13.6, but 14000 x 128 6.5 / 7.3; 4 % less on average.
     while (p.batch < 8 && 8 * p.batch * d <= 4096 && 4ll * p.batch * p.groups * sms * per_sm <= b) p.batch *= 2;
     p.blocks = std::min((b - 1) / (p.groups * p.batch) + 1, sms * per_sm);
     p.shared_bytes = per_sm > 1 ? kNormSharedBytes / 2 - 2048 : kNormSharedBytes;
     return p;
 }
-// Two blocks of 12 warps, so that one of them works while the other begins or ends, or one of 16, whose ring has two stages where those of two blocks
-// have one: for rows of which two do not fit in half the memory beside gamma and beta, and, with checkpoints, from 4096 on.  us, one block of 24 / two of 12:
-// 8192 x 768 with both checkpoints 25.6 / 22.2, 2039 x 5120 14.7 / 13.1, 4096 x 8192 49 / 53; one of 16 / two of 12: 4096 x 8192 50 / 53, with a
-// checkpoint of Y 16384 x 4096 140 / 144, 8192 x 5120 90.5 / 92.5, 4096 x 3584 34.9 / 34.2, 8192 x 768 18.8 / 16.8.  Up to 6144 one block of 24, which has four rows at a time
-// and not two: 4096 x 6144 with a checkpoint 61 / 42; 4096 x 8192 with residual and checkpoint 70 / 75.
-// An fp32 stream with a residual and without checkpoints moves 12 bytes per value and has little else to do: two chunks a lane, so that fewer rows are under
-// way at a time (two per SM at 4096), and rows that leave L2 like others.  us, as above / so: 8192 x 3584 63.8 / 57.8, 16384 x 4096 139 / 127 (98 % of a copy),
-// 8192 x 5120 91.5 / 83, 8192 x 6144 110 / 103, 8192 x 8192 139.5 / 127, 8192 x 2304 41.6 / 39.4, but 16384 x 2048 70 / 72.6; bf16 16384 x 4096 90 / 92, 8192 x 5120 59 / 82.
+// Two blocks of 12 warps, so that one of them works while the other begins or ends, or one of 16, whose ring has two stages where those of
+// two blocks have one: for rows of which two do not fit in half the memory beside gamma and beta, and, with checkpoints, from 4096 on.  us,
+// one block of 24 / two of 12: 8192 x 768 with both checkpoints 25.6 / 22.2, 2039 x 5120 14.7 / 13.1, 4096 x 8192 49 / 53; one of 16 / two
+// of 12: 4096 x 8192 50 / 53, with a checkpoint of Y 16384 x 4096 140 / 144, 8192 x 5120 90.5 / 92.5, 4096 x 3584 34.9 / 34.2, 8192 x 768
+// 18.8 / 16.8.  Up to 6144 one block of 24, which has four rows at a time and not two: 4096 x 6144 with a checkpoint 61 / 42; 4096 x 8192
+// with residual and checkpoint 70 / 75.
+// An fp32 stream with a residual and without checkpoints moves 12 bytes per value and has little else to do: two chunks a lane, so that
+// fewer rows are under way at a time (two per SM at 4096), and rows that leave L2 like others.  us, as above / so: 8192 x 3584 63.8 / 57.8,
+// 16384 x 4096 139 / 127 (98 % of a copy), 8192 x 5120 91.5 / 83, 8192 x 6144 110 / 103, 8192 x 8192 139.5 / 127, 8192 x 2304 41.6 / 39.4,
+// but 16384 x 2048 70 / 72.6; bf16 16384 x 4096 90 / 92, 8192 x 5120 59 / 82.
 static bool norm_fwd_heavy(int d, int x_type, bool residual, bool ckpt) {
     return x_type == SLOPE_F32 && residual && !ckpt && d > 2048 && d <= 8192;
 }
-// Wider than 8192: three chunks on up to 24 warps, two rows at a time up to 9216 (what a block's memory holds of an fp32 row with its residual, gamma and beta).
-// 4096 rows, us, four chunks on 16 warps / so: 8448 bf16 55 / 31, with residual and checkpoint 104 / 75, in fp32 114 / 97; 11008 57 / 55, 113 / 107, 133 / 128; 13824
-// 65 / 56.5, 130 / 116, 165 / 162; 16384 62 / 70, 142 / 143, 192 / 188.
+// Wider than 8192: three chunks on up to 24 warps, two rows at a time up to 9216 (what a block's memory holds of an fp32 row with its
+// residual, gamma and beta). 4096 rows, us, four chunks on 16 warps / so: 8448 bf16 55 / 31, with residual and checkpoint 104 / 75, in fp32
+// 114 / 97; 11008 57 / 55, 113 / 107, 133 / 128; 13824 65 / 56.5, 130 / 116, 165 / 162; 16384 62 / 70, 142 / 143, 192 / 188.
 static NormPlan norm_fwd_plan(int b, int d, bool heavy, bool ckpt, const DeviceInfo& info) {
     if (heavy) return norm_plan(b, d, 2, d <= 4096 ? 16 : kNormFwdWarps, 1, info.sm_count);
     if (d > 8192 && d <= 15 * 1024) return norm_plan(b, d, 3, kNormFwdWarps, 1, info.sm_count);
     const bool two = ckpt ? d < 4096 : d <= 5 * 1024;
     return norm_plan(b, d, 4, two ? kNormFwdWarps / 2 : d > 5120 && d <= 6144 ? kNormFwdWarps : 16, two ? 2 : 1, info.sm_count);
 }
-// One block of 16 warps per SM, or two of 8 where a row is one warp's: they begin and end apart.  Not for up to 16 rows, which one block takes without a second launch, nor
-// for many rows of at most 512.  us, one / two: 256 x 512 6.3 / 5.5, 2048 x 512 7.3 / 7.6, 8192 x 512 13.4 / 14.9,
-// 100 x 768 7.5 / 6.3, 2048 x 768 8.6 / 8.9, 16384 x 768 27.6 / 25.8, 32768 x 1024 55.3 / 54.8, 16 x 512 4.6 / 5.2.
-// Three chunks where four would have no more rows at a time: us, four / three, 4096 rows from 8 bits: 5376 48 / 44.5, 6144 55 / 48, 8448 83 / 70, 11008 90 / 86,
-// 12288 104 / 91; bf16 8448 75 / 65, 11008 82 / 83; fp32 12288 184 / 160.
+// One block of 16 warps per SM, or two of 8 where a row is one warp's: they begin and end apart.  Not for up to 16 rows, which one block
+// takes without a second launch, nor for many rows of at most 512.  us, one / two: 256 x 512 6.3 / 5.5, 2048 x 512 7.3 / 7.6, 8192 x 512
+// 13.4 / 14.9, 100 x 768 7.5 / 6.3, 2048 x 768 8.6 / 8.9, 16384 x 768 27.6 / 25.8, 32768 x 1024 55.3 / 54.8, 16 x 512 4.6 / 5.2.
+// Three chunks where four would have no more rows at a time: us, four / three, 4096 rows from 8 bits: 5376 48 / 44.5, 6144 55 / 48, 8448 83
+// / 70, 11008 90 / 86, 12288 104 / 91; bf16 8448 75 / 65, 11008 82 / 83; fp32 12288 184 / 160.
 // (The caller's workspace follows from the blocks and is asked for with no device at hand: the SM count is the B200's.)
 static NormPlan norm_bwd_plan(int b, int d) {
     const bool two = d <= 1024 && b > kNormBwdWarps && (d > 512 || b <= 1024);
@@ -61,12 +65,13 @@ static NormPlan norm_bwd_plan(int b, int d) {
     return norm_plan(b, d, most, two ? kNormBwdWarps / 2 : kNormBwdWarps, two ? 2 : 1, 148);
 }
 
-// The ring of a launch, gamma and beta behind it.  `leave_first`: us, rows leave L2 first / like others: forward 16384 x 4096 90 / 95, in fp32 139 / 147; but
-// with a checkpoint of Y (written and then read back) 140 / 136, in fp32 189 / 181.
-static NormRing norm_ring(const NormPlan& plan, int b, int d, bool leave_first, const void* gamma, const void* beta, int params, int p_type, const void* s0, int bytes0,
-                          const void* s1, int bytes1, const void* s2, int bytes2) {
+// The ring of a launch, gamma and beta behind it.  `leave_first`: us, rows leave L2 first / like others: forward 16384 x 4096 90 / 95, in
+// fp32 139 / 147; but with a checkpoint of Y (written and then read back) 140 / 136, in fp32 189 / 181.
+static NormRing norm_ring(const NormPlan& plan, int b, int d, bool leave_first, const void* gamma, const void* beta, int params, int p_type,
+                          const void* s0, int bytes0, const void* s1, int bytes1, const void* s2, int bytes2) {
     NormRing r{{static_cast<const uint8_t*>(s0), static_cast<const uint8_t*>(s1), static_cast<const uint8_t*>(s2)},
-               {bytes0, s1 ? bytes1 : 0, s2 ? bytes2 : 0}, plan.batch, 0, plan.groups, plan.row_warps, b, d, leave_first, {gamma, beta}, p_type == SLOPE_F32, params};
+               {bytes0, s1 ? bytes1 : 0, s2 ? bytes2 : 0}, plan.batch, 0, plan.groups, plan.row_warps, b, d, leave_first, {gamma, beta},
+               p_type == SLOPE_F32, params};
     r.stages = std::max(1, std::min(kNormMaxStages, (plan.shared_bytes - r.param_bytes()) / (r.groups * r.stage_bytes())));
     return r;
 }
@@ -97,8 +102,10 @@ template <int TYPE, int DX_TYPE, int CHUNKS>
 static slope_status_t launch_norm_bwd_of(const NormPlan& plan, const NormBwdParams& p, cudaStream_t stream) {
     const bool full = p.ring.d == 256 * plan.row_warps * CHUNKS, side = p.ring.src[2];
     // (the groups' sums of the parameters' gradients take the place of the ring in the end)
-    return launch_norm(full ? (side ? layer_norm_bwd_kernel<TYPE, DX_TYPE, CHUNKS, true, true> : layer_norm_bwd_kernel<TYPE, DX_TYPE, CHUNKS, true, false>)
-                            : side ? layer_norm_bwd_kernel<TYPE, DX_TYPE, CHUNKS, false, true> : layer_norm_bwd_kernel<TYPE, DX_TYPE, CHUNKS, false, false>,
+    return launch_norm(full ? (side ? layer_norm_bwd_kernel<TYPE, DX_TYPE, CHUNKS, true, true>
+                                    : layer_norm_bwd_kernel<TYPE, DX_TYPE, CHUNKS, true, false>)
+                            : side ? layer_norm_bwd_kernel<TYPE, DX_TYPE, CHUNKS, false, true>
+                                   : layer_norm_bwd_kernel<TYPE, DX_TYPE, CHUNKS, false, false>,
                        plan, plan.groups * 8 * p.ring.d, stream, p);
 }
 template <int TYPE, int DX_TYPE>
@@ -153,8 +160,9 @@ slope_status_t slope_layer_norm_fwd(const void* X, int x_type, const void* resid
     if (slope_status_t st = check_arch(info)) return st;
     const bool ckpt = H_ckpt || Y_ckpt, heavy = norm_fwd_heavy(d, x_type, residual, ckpt);
     const NormPlan plan = norm_fwd_plan(b, d, heavy, ckpt, info);
-    const NormFwdParams p{norm_ring(plan, b, d, !ckpt && !heavy, gamma, beta, 2, p_type, X, x_type == SLOPE_F32 ? 4 * d : 2 * d, residual, 2 * d, nullptr, 0), H, Y, H_ckpt, Y_ckpt,
-                          static_cast<float*>(mean), static_cast<float*>(rstd), eps};
+    const int x_bytes = x_type == SLOPE_F32 ? 4 * d : 2 * d;
+    const NormFwdParams p{norm_ring(plan, b, d, !ckpt && !heavy, gamma, beta, 2, p_type, X, x_bytes, residual, 2 * d, nullptr, 0), H, Y,
+                          H_ckpt, Y_ckpt, static_cast<float*>(mean), static_cast<float*>(rstd), eps};
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     return x_type == SLOPE_F32 ? launch_norm_fwd<kTypeF32>(plan, p, stream) : launch_norm_fwd<kTypeBf16>(plan, p, stream);
 }
@@ -181,14 +189,17 @@ slope_status_t slope_layer_norm_bwd(const void* dY, const void* H, int h_type, c
     if (slope_status_t st = check_arch(info)) return st;
     const NormPlan plan = norm_bwd_plan(b, d);
     const int h_bytes = h_type == SLOPE_F32 ? 4 * d : h_type == SLOPE_Q8 ? d : 2 * d;
-    const NormBwdParams p{norm_ring(plan, b, d, true, gamma, nullptr, plan.chunks > 2, p_type, H, h_bytes, dY, 2 * d, dH, dx_type == SLOPE_F32 ? 4 * d : 2 * d),
+    const int dx_bytes = dx_type == SLOPE_F32 ? 4 * d : 2 * d;
+    const NormBwdParams p{norm_ring(plan, b, d, true, gamma, nullptr, plan.chunks > 2, p_type, H, h_bytes, dY, 2 * d, dH, dx_bytes),
                           static_cast<const uint8_t*>(H) + static_cast<size_t>(b) * d, static_cast<const float*>(mean),
                           static_cast<const float*>(rstd), dX, dgamma, dbeta, static_cast<float*>(workspace)};
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     const bool wide = dx_type == SLOPE_F32;
     slope_status_t st;
-    if (h_type == SLOPE_BF16) st = wide ? launch_norm_bwd<kTypeBf16, kTypeF32>(plan, p, stream) : launch_norm_bwd<kTypeBf16, kTypeBf16>(plan, p, stream);
-    else if (h_type == SLOPE_F32) st = wide ? launch_norm_bwd<kTypeF32, kTypeF32>(plan, p, stream) : launch_norm_bwd<kTypeF32, kTypeBf16>(plan, p, stream);
+    if (h_type == SLOPE_BF16)
+        st = wide ? launch_norm_bwd<kTypeBf16, kTypeF32>(plan, p, stream) : launch_norm_bwd<kTypeBf16, kTypeBf16>(plan, p, stream);
+    else if (h_type == SLOPE_F32)
+        st = wide ? launch_norm_bwd<kTypeF32, kTypeF32>(plan, p, stream) : launch_norm_bwd<kTypeF32, kTypeBf16>(plan, p, stream);
     else st = wide ? launch_norm_bwd<kTypeQ8, kTypeF32>(plan, p, stream) : launch_norm_bwd<kTypeQ8, kTypeBf16>(plan, p, stream);
     if (st != SLOPE_OK || !params || plan.blocks == 1) return st;
     return launch_cluster_ex(layer_norm_params_kernel, (2 * d + 31) / 32, 1, 256, 0, /*overlap_prologue=*/true, stream, p.partial, plan.blocks, d,

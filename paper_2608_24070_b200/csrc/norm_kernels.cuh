@@ -218,10 +218,11 @@ __global__ void __launch_bounds__(256) checkpoint_load_kernel(const void* ckpt, 
 // per SM) cost no registers.  A stage holds `batch` adjacent rows (several where they are short), one copy per matrix; the group's first lane
 // asks for the next ones when the group has read it.  Groups have nothing to do with one another.
 //
-// What bounds them: HBM for long rows (16384 x 4096: forward 6.0, backward 5.6 of 6.45 TB/s), else what is issued and waited for per row: at HBM's
-// rate an SM has 890 clocks for a row of 5120 values.  us of the forward of 8192 x 5120 with fp32 parameters, 168 MB (floor 26), as it went: rows loaded by
-// the warps, one fp32 value per instruction 62; the same from the ring, instances without branches on what a call leaves out, two values per
-// instruction (23.6 -> 11.6 instructions per value) 43; 24 warps instead of 16 37; loads that leave L2 first 35.
+// What bounds them: HBM for long rows (16384 x 4096: forward 6.0, backward 5.6 of 6.45 TB/s), else what is issued and waited for per row:
+// at HBM's rate an SM has 890 clocks for a row of 5120 values.  us of the forward of 8192 x 5120 with fp32 parameters, 168 MB (floor 26),
+// as it went: rows loaded by the warps, one fp32 value per instruction 62; the same from the ring, instances without branches on what a
+// call leaves out, two values per instruction (23.6 -> 11.6 instructions per value) 43; 24 warps instead of 16 37; loads that leave L2
+// first 35.
 constexpr int kNormMaxWidth = 16384;
 constexpr int kNormFwdWarps = 24, kNormBwdWarps = 16;             // of a block at most: so many as leave a row its registers
 constexpr int kNormWarps = kNormFwdWarps;
@@ -627,11 +628,12 @@ __device__ __forceinline__ void store_param(void* base, bool f32, int at, float 
 }
 
 // gamma's and beta's gradients grow in registers; at the end the groups' sums meet in shared memory (where the ring was) and are added in
-// order, and the blocks' sums are added in order by layer_norm_params_kernel (a single block writes the gradients itself).  The order depends on
-// the sizes alone.
-// Registers are what it is short of: four chunks' sums take 64, so that from three chunks on a row's values are not kept between its two sums and its
-// output but read from the ring and normalised again.  us, one / two (kept) / four (read again) chunks per lane: 16384 x 4096 140 / 94 / 94, 8192 x 5120 from
-// 8 bits 76 / 98 / 76, 4096 x 8192 56 / 58 / 56, 8192 x 768 from 8 bits 18.9 / 21 / 18.9 (three chunks).
+// order, and the blocks' sums are added in order by layer_norm_params_kernel (a single block writes the gradients itself).  The order
+// depends on the sizes alone.
+// Registers are what it is short of: four chunks' sums take 64, so that from three chunks on a row's values are not kept between its two
+// sums and its output but read from the ring and normalised again.  us, one / two (kept) / four (read again) chunks per lane: 16384 x 4096
+// 140 / 94 / 94, 8192 x 5120 from 8 bits 76 / 98 / 76, 4096 x 8192 56 / 58 / 56, 8192 x 768 from 8 bits 18.9 / 21 / 18.9 (three chunks).
+// At 128 registers ten of the 96 instances spill 4 to 48 bytes (the full one of four chunks in bf16 with dH 12, from 8 bits 44).
 template <int TYPE, int DX_TYPE, int CHUNKS, bool FULL, bool SIDE>
 __global__ void __launch_bounds__(32 * kNormBwdWarps, 1) layer_norm_bwd_kernel(const __grid_constant__ NormBwdParams p) {
     constexpr bool kReread = CHUNKS > 2;      // a row does not fit in registers beside its columns' sums: it is read from the ring twice
