@@ -48,6 +48,13 @@ def test_no_copy_in_bf16_is_saved(H, r):  # noqa: F811
     assert saved[True] == sorted(statistics + kept + codes)
 
 
+def requested(which):
+    """Bytes that were asked for.  (What the allocator counts as allocated depends on what ran before: a block of which less than 1 MB would be left is not split.)"""
+    import torch
+
+    return torch.cuda.memory_stats()[f"requested_bytes.all.{which}"]
+
+
 def held(H, r, checkpoint, blocks=4, tokens=4096):  # noqa: F811
     """Bytes beyond the model's own: behind the second step's forward pass, when that step is over, and at its peak."""
     import torch
@@ -56,27 +63,28 @@ def held(H, r, checkpoint, blocks=4, tokens=4096):  # noqa: F811
     layers = [model(H, r, checkpoint)[:2] for _ in range(blocks)]
     x = B.bf16_from_bits(si.gaussian_bf16((tokens, D), 1.0, 5302))
     torch.cuda.synchronize()
-    start = torch.cuda.memory_allocated()
+    start = requested("current")
     for _ in range(2):
         torch.cuda.reset_peak_memory_stats()
         out = x.detach().requires_grad_(True)
         for gpu, norms in layers:
             out = forward(gpu, norms, out)
-        behind_forward = torch.cuda.memory_allocated() - start
+        behind_forward = requested("current") - start
         out.sum().backward()
         del out
-    return behind_forward, torch.cuda.memory_allocated() - start, torch.cuda.max_memory_allocated() - start
+    return behind_forward, requested("current") - start, requested("peak") - start
 
 
 @pytest.mark.parametrize("r", [0, 64])
 def test_steps_with_checkpoints_hold_less(H, r):  # noqa: F811
     """A block saves five matrices of [tokens x d] and one of [tokens x ffn], 31 / 64 of which checkpoints spare (the first block's stream is the
-    caller's input, which stays); the backward pass adds one decoded matrix at a time."""
+    caller's input, which stays, so that its codes come on top: with what the caller holds of the last output the difference is exact); the backward
+    pass adds one decoded matrix at a time, and the other workspaces are below 16 MB."""
     blocks, tokens = 4, 4096
     off, on = held(H, r, False, blocks, tokens), held(H, r, True, blocks, tokens)
     print("bytes behind the forward pass, behind the step, at the peak:", off, on)
     spared = blocks * 31 * 2 * tokens * (5 * D + FFN) // 64 - 2 * tokens * D
-    assert on[0] <= off[0] - spared
+    assert on[0] == off[0] - spared if r == 0 else on[0] <= off[0] - spared
     assert on[1] == 0
     assert on[2] <= off[2] - spared + 2 * tokens * FFN + (1 << 24)
 
