@@ -177,3 +177,25 @@ def test_rows_next_to_the_range_do_not_depend_on_others(B, d, x):  # noqa: F811
         for first in range(6):                       # equal rows of one call, wherever they stand
             assert (alone[k][first::6] == alone[k][first]).all(), k
     assert torch.isfinite(out["Y"]).all() and (out["rstd"] > 0).all()
+
+
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 768, 5120])
+def test_one_large_value_in_an_ordinary_row(B, d, x):  # noqa: F811
+    """A single value next to the type's largest number: its square leaves fp32, the row's other values stand at next to nothing beside it."""
+    import torch
+
+    c = case(9, d, x, "f32", d, residual=True)
+    c["X"][6, 33] = -0.99 * torch.finfo(c["X"].dtype).max
+    out = forward(B, c, 1e-5, ckpt=True)
+    h = f64(out["H"])
+    y, mean, rstd, xhat = ref.layer_norm(h, f64(c["gamma"]), f64(c["beta"]), 1e-5)
+    e_mean = U * ADDS * np.abs(h).mean(-1)
+    lean = e_mean * rstd
+    e_rstd = rstd * (U * (ADDS + 8) / 2 + 2 * U + lean * lean) + 2.0 ** -150
+    within(f64(out["mean"]), mean, e_mean + U * np.abs(mean), "mean")
+    within(f64(out["rstd"]), rstd, e_rstd, "rstd")
+    gamma, beta = np.abs(f64(c["gamma"])), np.abs(f64(c["beta"]))
+    e_y = gamma * (lean[:, None] + np.abs(xhat) * (e_rstd / rstd + 3 * U)[:, None]) + 2 * U * (gamma * np.abs(xhat) + beta)
+    within(f64(out["Y"]), y, e_y * (1 + HALF["bf16"]) + HALF["bf16"] * np.abs(y), "Y")
+    assert np.array_equal(out["Yc"].cpu().numpy(), ref.buffer(*ref.encode(f64(out["Y"]))))
