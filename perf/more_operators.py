@@ -70,10 +70,12 @@ def draw(rng):
                 "base": rng.choice([10000.0, 500000.0]), "stretch": rng.choice([1.0, 1.0, 4.0, 8.0]), "offset": rng.choice([0, 0, 4000, 1000000])}
     batch = rng.choice(["equal", "equal", "padded", "packed"])
     seqs = round(_log_uniform(rng, 1, 32))
-    longest = min(16384 / seqs, math.sqrt(2 * _MOST / (heads * hd * seqs)) if seqs else 1)
-    length = max(1, round(_log_uniform(rng, 1, longest)))
+    longest = min(16384 / seqs, math.sqrt(2 * _MOST / (heads * hd * seqs)))
+    # (a token that sees itself alone has gradients of exactly zero for its query and key: nothing that could be compared relative to its size)
+    least = 1 if kind == "attn_fwd" else 8
+    length = max(least, round(_log_uniform(rng, least, longest)))
     causal = rng.random() < 0.7
-    window = round(_log_uniform(rng, 1, 2 * length)) if causal and rng.random() < 0.3 else 0
+    window = round(_log_uniform(rng, least, 2 * length)) if causal and rng.random() < 0.3 else 0
     return {"kind": kind, "seqs": seqs, "len": length, "heads": heads, "kv": kv, "hd": hd, "causal": causal, "window": window, "batch": batch}
 
 
