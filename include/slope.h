@@ -360,6 +360,55 @@ slope_status_t slope_dense_linear_bwd_dw_q8(const void* dY, const void* X_ckpt, 
                                             void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Rotation of queries and keys by their positions.  Of the rot_dim = 2 n first columns of every head (head_dim a multiple of 8, rot_dim even), each pair
+ * (u_i, v_i) becomes
+ *   factor (u cos a - v sin a, v cos a + u sin a),   a = positions[row] * frequencies[i]
+ * the other columns stay as they are.  Pairs are columns (i, n + i) or, interleaved != 0, (2 i, 2 i + 1).  backward != 0: the transposed map, which
+ * takes the gradients of the rotated queries and keys back.
+ *   Q, K          [b x heads * head_dim], [b x kv_heads * head_dim] of `type` (SLOPE_BF16 or SLOPE_F32), rows `*_ld` elements apart (a multiple
+ *                 of 8); K and Kr may be NULL
+ *   positions     int32 [b], any values;  frequencies: fp64 [n], radians a position (how they are scaled for long contexts is the caller's)
+ *   Qr, Kr        results: other memory, or Q and K themselves (both, at the same row strides)
+ * Angles are reduced in fp64: exact to 1e-7 of a turn at any position.
+ */
+slope_status_t slope_rotary(const void* Q, int q_ld, const void* K, int k_ld, int type, int b, int heads, int kv_heads, int head_dim, int rot_dim,
+                            int interleaved, int backward, const void* positions, const void* frequencies, float factor, void* Qr, int qr_ld,
+                            void* Kr, int kr_ld, void* stream);
+
+/*
+ * Softmax attention between the linear layers (their Y is its input, its output their X), row-major as they have it: Q, O [b x heads *
+ * head_dim], K, V [b x kv_heads * head_dim], bf16, rows `*_ld` elements apart (so that Q, K and V may be columns of one matrix):
+ *   O = softmax(scale Q K^T) V   per sequence and head;   lse = log of the sum of exp(scale Q K^T), fp32 [heads x b] (NULL: not wanted)
+ * head_dim a multiple of 8 up to 128; heads a multiple of kv_heads: heads / kv_heads query heads in a row share a key head.
+ *   sequences, starts   starts (int32 [sequences + 1], device, or NULL): sequence i has rows starts[i] ... starts[i + 1] - 1; NULL: b is a
+ *                       multiple of `sequences`, which are equally long
+ *   lengths             int32 [sequences], device, or NULL: sequence i has no more than that many of its rows (a padded batch)
+ *   causal, window      a token sees its own sequence, with causal != 0 itself and the tokens before it, with window > 0 (causal only) no more
+ *                       than the last `window` of these, itself among them
+ * Rows of no sequence are not written, and what they hold reaches no other row; a sequence may have length 0.  Starts are ascending and within
+ * [0, b]; others are held to that range (no access is out of bounds, the results are not defined).  An infinity or a NaN shows in
+ * the rows that see it as the formula has it (a score of minus infinity is a probability of 0, one of plus infinity a row of NaN); one in V (for the
+ * gradients: in any input) may also make rows NaN that have it in the same tile of 128 as their causal border or the end of their window.  Probabilities are rounded to bf16 for the second product; sums are fp32.  Outputs must not overlap inputs or one another.
+ */
+slope_status_t slope_attention_fwd(const void* Q, int q_ld, const void* K, int k_ld, const void* V, int v_ld, int b, int heads, int kv_heads,
+                                   int head_dim, int sequences, const void* starts, const void* lengths, int causal, int window, float scale,
+                                   void* O, int o_ld, void* lse, void* stream);
+
+/*
+ * Its backward pass: the probabilities P = exp(scale Q K^T - lse) are formed once more, and with D = sum over a head's columns of dO O
+ *   dV = P^T dO,   dS = P (dO V^T - D),   dQ = scale dS K,   dK = scale dS^T Q,
+ * dK and dV summed over the heads that share a key head.  O and lse are those of slope_attention_fwd.  P and dS are rounded to bf16 for the
+ * products behind them; all sums are fp32 and have a fixed order.  Rows of no sequence are not written.  `workspace`: device scratch of at least
+ * slope_attention_bwd_workspace_bytes() bytes.
+ */
+size_t slope_attention_bwd_workspace_bytes(int b, int heads, int kv_heads, int head_dim);
+slope_status_t slope_attention_bwd(const void* dO, int do_ld, const void* Q, int q_ld, const void* K, int k_ld, const void* V, int v_ld,
+                                   const void* O, int o_ld, const void* lse, int b, int heads, int kv_heads, int head_dim, int sequences,
+                                   const void* starts, const void* lengths, int causal, int window, float scale,
+                                   void* dQ, int dq_ld, void* dK, int dk_ld, void* dV, int dv_ld,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Diagnostic: rewrite tensor-core-order metadata as canonical metadata
  * (uint16 [rows x cols/16], group g of a row at bits 4*(g%4) of unit g/4).
  * Paper counterpart: none (the index storage of Eq. (index_bits) in a

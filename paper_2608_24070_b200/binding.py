@@ -39,6 +39,7 @@ EXPORTS = (
     "slope_layer_norm_fwd", "slope_layer_norm_bwd_workspace_bytes", "slope_layer_norm_bwd",
     "slope_bwd_dw_q8_workspace_bytes", "slope_linear_bwd_dw_masked_q8", "slope_linear_bwd_dw_adapter_q8",
     "slope_dense_linear_bwd_dw_q8",
+    "slope_rotary", "slope_attention_fwd", "slope_attention_bwd_workspace_bytes", "slope_attention_bwd",
 )
 
 
@@ -108,9 +109,13 @@ def lib() -> ctypes.CDLL:
             "slope_linear_bwd_dw_masked_q8": [vp, vp, ci, ci, ci, vp, vp, vp, sz, vp],
             "slope_linear_bwd_dw_adapter_q8": [vp, vp, vp, vp, ci, ci, ci, ci, vp, vp, vp, vp, vp, sz, vp],
             "slope_dense_linear_bwd_dw_q8": [vp, vp, ci, ci, ci, vp, vp, sz, vp],
+            "slope_rotary": [vp, ci, vp, ci, ci, ci, ci, ci, ci, ci, ci, ci, vp, vp, ctypes.c_float, vp, ci, vp, ci, vp],
+            "slope_attention_fwd": [vp, ci] * 3 + [ci] * 5 + [vp, vp, ci, ci, ctypes.c_float, vp, ci, vp, vp],
+            "slope_attention_bwd": [vp, ci] * 5 + [vp] + [ci] * 5 + [vp, vp, ci, ci, ctypes.c_float] + [vp, ci] * 3 + [vp, sz, vp],
         }.items():
             getattr(L, name).argtypes, getattr(L, name).restype = args, ci
-        for name, count in {"slope_checkpoint_bytes": 2, "slope_layer_norm_bwd_workspace_bytes": 2, "slope_bwd_dw_q8_workspace_bytes": 4}.items():
+        for name, count in {"slope_checkpoint_bytes": 2, "slope_layer_norm_bwd_workspace_bytes": 2, "slope_bwd_dw_q8_workspace_bytes": 4,
+                            "slope_attention_bwd_workspace_bytes": 4}.items():
             getattr(L, name).argtypes, getattr(L, name).restype = [ci] * count, sz
         L.slope_poll_status.argtypes = [vp]
         L.slope_kernel_clock_mhz.argtypes = [ci, vp, ctypes.POINTER(ctypes.c_double)]
@@ -350,6 +355,39 @@ def slope_dense_linear_bwd_dw_q8(dY, X_ckpt, dW, workspace=None):
         _check("slope_dense_linear_bwd_dw_q8", st)
 
 
+def slope_rotary(Q, K, positions, frequencies, head_dim, Qr, Kr, factor=1.0, interleaved=False, backward=False):
+    """Qr, Kr: queries and keys turned by their positions (backward: gradients turned back).  K and Kr may be None; Qr and Kr may be Q and K.
+    Rows may be further apart than they are long (columns of a wider matrix), here and in the attention calls."""
+    st = (_native or _calls()).slope_rotary(Q, K, positions, frequencies, head_dim, Qr, Kr, factor, interleaved, backward)
+    if st:
+        _check("slope_rotary", st)
+
+
+def slope_attention_fwd(Q, K, V, head_dim, O, lse=None, sequences=None, starts=None, lengths=None, causal=True, window=0, scale=None):
+    """O = softmax(scale Q K^T) V per sequence and head; lse [heads x b]: what the backward pass needs.  scale None: 1 / sqrt(head_dim);
+    sequences None: as many as the starts say, or one."""
+    if sequences is None:
+        sequences = 1 if starts is None else starts.numel() - 1
+    st = (_native or _calls()).slope_attention_fwd(Q, K, V, head_dim, O, lse, sequences, starts, lengths, causal, window,
+                                                   head_dim ** -0.5 if scale is None else scale)
+    if st:
+        _check("slope_attention_fwd", st)
+
+
+def slope_attention_bwd_workspace_bytes(b: int, heads: int, kv_heads: int, head_dim: int) -> int:
+    return int(lib().slope_attention_bwd_workspace_bytes(b, heads, kv_heads, head_dim))
+
+
+def slope_attention_bwd(dO, Q, K, V, O, lse, head_dim, dQ, dK, dV, workspace, sequences=None, starts=None, lengths=None, causal=True, window=0,
+                        scale=None):
+    if sequences is None:
+        sequences = 1 if starts is None else starts.numel() - 1
+    st = (_native or _calls()).slope_attention_bwd(dO, Q, K, V, O, lse, head_dim, dQ, dK, dV, workspace, sequences, starts, lengths, causal, window,
+                                                   head_dim ** -0.5 if scale is None else scale)
+    if st:
+        _check("slope_attention_bwd", st)
+
+
 def slope_mask_difference(mask_a, mask_b, count_out):
     rows, mrow = mask_a.shape
     _check("slope_mask_difference", lib().slope_mask_difference(_ptr(mask_a), _ptr(mask_b), rows, mrow * 8,
@@ -410,6 +448,30 @@ def alloc_checkpoint(rows: int, cols: int, device="cuda"):
     if nbytes == 0:
         raise ValueError("a checkpoint has at least one row and a multiple of 32 columns")
     return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def rotary_frequencies(rot_dim: int, base: float = 10000.0, scaling: Optional[str] = None, stretch: float = 1.0, trained: int = 4096,
+                       fast: float = 32.0, slow: float = 1.0, device="cuda") -> torch.Tensor:
+    """Radians a position of the rot_dim / 2 pairs, fp64: base^(-2 i / rot_dim), or scaled for a context `stretch` times the `trained` one.
+
+    "linear": all divided by the stretch; "base": the base raised by stretch^(rot_dim / (rot_dim - 2)), which divides the slowest by the stretch
+    and leaves the fastest; "parts": pairs that turn more than `fast` times within the trained context stay, those that turn less than `slow`
+    times are divided by the stretch, with a ramp over the number of turns between them."""
+    if rot_dim < 2 or rot_dim % 2 or not base > 0 or not stretch > 0 or scaling not in (None, "linear", "base", "parts"):
+        raise ValueError("rotary_frequencies: an even number of columns, a positive base and stretch, scaling None, linear, base or parts")
+    if scaling == "base":
+        if rot_dim < 4:
+            raise ValueError("rotary_frequencies: a single pair has no slowest and fastest")
+        base *= stretch ** (rot_dim / (rot_dim - 2))
+    f = base ** (-2.0 * torch.arange(rot_dim // 2, dtype=torch.float64) / rot_dim)
+    if scaling == "linear":
+        f = f / stretch
+    if scaling == "parts":
+        if not fast > slow:
+            raise ValueError("rotary_frequencies: fast must be above slow")
+        kept = ((trained * f / (2.0 * torch.pi) - slow) / (fast - slow)).clamp(0.0, 1.0)
+        f = f * (kept + (1.0 - kept) / stretch)
+    return f.to(device)
 
 
 def bf16_from_bits(bits, device="cuda") -> torch.Tensor:

@@ -5,7 +5,7 @@ torch autograd by a ``torch.autograd.Function`` whose backward issues the adapte
 input gradient with the doubly pruned weight and the masked compressed weight gradient
 (Eq. (sparse_forward), Eq. (sparse_backward_input), Eq. (sparse_backward_weight), Eq. (concat)).
 Everything between them -- RMS normalisation without gain, causal attention without positional
-rotation, the SiLU gate, the residual adds -- is plain torch in bf16 and is NOT part of the
+rotation, the SiLU gate, the residual adds -- is by default plain torch in bf16 and is then NOT part of the
 library: it is there so that the linears see a real data flow, each one fed by the previous
 one's output and its gradient by the next one's.  ``DenseLinear`` is the same block on
 ``torch.nn.functional.linear`` (cuBLAS) for the all-dense comparison.
@@ -16,6 +16,9 @@ stream, the linears of their inputs; linears that share an input share its check
 Their calls' workspaces (a decoded matrix of activations among them) are allocated for the one call and go back to torch's caching
 allocator behind it, so that all layers of a model use the same memory in turn and nothing stays; what a captured graph needs comes from
 that graph's own pool.
+
+With ``attention`` queries and keys are turned by their positions and attention runs on the library's calls (``Attention``): shared key
+heads, windows, packed and padded batches.
 
 Every linear call is bracketed by CUDA events when ``timers`` is given, so the time spent in
 the linears can be summed separately from the torch glue.
@@ -144,18 +147,19 @@ class _SlopeLinearFn(torch.autograd.Function):
 
 class _FirstDerivativeFn(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, gradient):
+    def forward(ctx, gradient, of):
+        ctx.of = of
         return gradient.view_as(gradient)
 
     @staticmethod
     def backward(ctx, _):
-        raise RuntimeError("LayerNorm has no second derivative")
+        raise RuntimeError(f"{ctx.of} has no second derivative")
 
 
-def _first_derivative(gradient: torch.Tensor) -> torch.Tensor:
+def _first_derivative(gradient: torch.Tensor, of: str) -> torch.Tensor:
     """A gradient that depends on inputs as well as on the gradient that came in: where a graph of the backward pass is asked for, going back
     through it is an error, instead of a derivative that lacks this part."""
-    return _FirstDerivativeFn.apply(gradient.requires_grad_(True)) if torch.is_grad_enabled() else gradient
+    return _FirstDerivativeFn.apply(gradient.requires_grad_(True), of) if torch.is_grad_enabled() else gradient
 
 
 class LayerNorm:
@@ -203,9 +207,59 @@ class _LayerNormFn(torch.autograd.Function):
         dX = torch.empty(b, d, dtype=ctx.dtype, device=dY.device)
         workspace = _scratch(B.slope_layer_norm_bwd_workspace_bytes(b, d), dY.device)
         B.slope_layer_norm_bwd(dY, H, mean, rstd, norm.gamma, dX, norm.dgamma, norm.dbeta, workspace, None if dH is None else dH.contiguous())
-        dX = _first_derivative(dX)
+        dX = _first_derivative(dX, "LayerNorm")
         # (the residual is a sub-layer's bf16 output, whatever the stream's type)
         return dX, dX.to(torch.bfloat16) if ctx.with_residual else None, None
+
+
+class Attention:
+    """Softmax attention over the library's calls, behind the rotation of queries and keys by their positions if there are ``frequencies``
+    (``binding.rotary_frequencies``).  A call takes the three projections' outputs [tokens x heads * head_dim] and says where the sequences lie;
+    ``positions`` int32 [tokens].  Rows of no sequence have an output and gradients of zero."""
+
+    def __init__(self, heads: int, kv_heads: Optional[int] = None, frequencies: Optional[torch.Tensor] = None, factor: float = 1.0,
+                 interleaved: bool = False, causal: bool = True, window: int = 0, scale: Optional[float] = None):
+        self.heads, self.kv_heads = heads, heads if kv_heads is None else kv_heads
+        self.frequencies, self.factor, self.interleaved = frequencies, factor, interleaved
+        self.mask = {"causal": causal, "window": window, "scale": scale}
+
+    def __call__(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, sequences: Optional[int] = None, starts: Optional[torch.Tensor] = None,
+                 lengths: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None) -> torch.Tensor:
+        if (self.frequencies is None) != (positions is None):
+            raise ValueError("Attention: positions and frequencies belong together")
+        return _AttentionFn.apply(q, k, v, self, {"sequences": sequences, "starts": starts, "lengths": lengths, **self.mask}, positions)
+
+
+class _AttentionFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, layer: Attention, batch, positions):
+        b, head_dim = q.shape[0], q.shape[1] // layer.heads
+        if q.shape[1] % layer.heads or k.shape[1] != layer.kv_heads * head_dim:
+            raise ValueError("Attention: the projections do not have these heads")
+        if positions is not None:
+            turned = torch.empty_like(q, memory_format=torch.contiguous_format), torch.empty_like(k, memory_format=torch.contiguous_format)
+            B.slope_rotary(q, k, positions, layer.frequencies, head_dim, *turned, factor=layer.factor, interleaved=layer.interleaved)
+            q, k = turned
+        # (rows of no sequence are not written)
+        ctx.fresh = torch.empty if batch["starts"] is None and batch["lengths"] is None else torch.zeros
+        O = ctx.fresh(b, layer.heads * head_dim, dtype=q.dtype, device=q.device)
+        lse = torch.empty(layer.heads, b, dtype=torch.float32, device=q.device)
+        B.slope_attention_fwd(q, k, v, head_dim, O, lse, **batch)
+        ctx.layer, ctx.batch, ctx.positions, ctx.head_dim = layer, batch, positions, head_dim
+        ctx.save_for_backward(q, k, v, O, lse)
+        return O
+
+    @staticmethod
+    def backward(ctx, dO):
+        layer: Attention = ctx.layer
+        q, k, v, O, lse = ctx.saved_tensors
+        grads = [ctx.fresh(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v)]
+        workspace = _scratch(B.slope_attention_bwd_workspace_bytes(q.shape[0], layer.heads, layer.kv_heads, ctx.head_dim), q.device)
+        B.slope_attention_bwd(dO.contiguous(), q, k, v, O, lse, ctx.head_dim, *grads, workspace, **ctx.batch)
+        if ctx.positions is not None:
+            dq, dk = grads[:2]
+            B.slope_rotary(dq, dk, ctx.positions, layer.frequencies, ctx.head_dim, dq, dk, factor=layer.factor, interleaved=layer.interleaved, backward=True)
+        return (*(_first_derivative(g, "Attention") for g in grads), None, None, None)
 
 
 class DenseLinear:
@@ -246,27 +300,33 @@ def causal_attention(q, k, v, batch: int, seq: int, heads: int) -> torch.Tensor:
 
 
 def decoder_block(x: torch.Tensor, layers: Dict[str, object], batch: int, seq: int, heads: int,
-                  eps: float = 1e-5, norms: Optional[Dict[str, LayerNorm]] = None) -> torch.Tensor:
+                  eps: float = 1e-5, norms: Optional[Dict[str, LayerNorm]] = None, attention: Optional[Attention] = None,
+                  positions: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x [batch*seq, d] bf16 -> block output [batch*seq, d] bf16; ``layers`` maps the seven names to callables, ``norms`` "attention"
-    and "mlp" to layer norms (None: RMS normalisation in torch)."""
+    and "mlp" to layer norms (None: RMS normalisation in torch).  ``attention`` with its ``positions`` takes the place of torch's."""
+    if attention is None:
+        attend = lambda q, k, v: causal_attention(q, k, v, batch, seq, heads)
+    else:
+        attend = lambda q, k, v: attention(q, k, v, sequences=batch, positions=positions)
     if norms is None:
         n1 = rms_norm(x, eps)
-        a = causal_attention(layers["q"](n1), layers["k"](n1), layers["v"](n1), batch, seq, heads)
+        a = attend(layers["q"](n1), layers["k"](n1), layers["v"](n1))
         h = x + layers["o"](a)
         n2 = rms_norm(h, eps)
         g = F.silu(layers["gate"](n2)) * layers["up"](n2)
         return h + layers["down"](g)
     x, n1, kept = norms["attention"](x)
-    a = causal_attention(layers["q"](n1, kept), layers["k"](n1, kept), layers["v"](n1, kept), batch, seq, heads)
+    a = attend(layers["q"](n1, kept), layers["k"](n1, kept), layers["v"](n1, kept))
     h, n2, kept = norms["mlp"](x, layers["o"](a))
     g = F.silu(layers["gate"](n2, kept)) * layers["up"](n2, kept)
     return h + layers["down"](g)
 
 
 def block_step(x: torch.Tensor, dout: torch.Tensor, layers: Dict[str, object], batch: int, seq: int, heads: int,
-               eps: float = 1e-5, norms: Optional[Dict[str, LayerNorm]] = None):
+               eps: float = 1e-5, norms: Optional[Dict[str, LayerNorm]] = None, attention: Optional[Attention] = None,
+               positions: Optional[torch.Tensor] = None):
     """One training step of the block for the loss <out, dOut> (no optimizer): returns (out, dx)."""
     x = x.detach().requires_grad_(True)
-    out = decoder_block(x, layers, batch, seq, heads, eps, norms)
+    out = decoder_block(x, layers, batch, seq, heads, eps, norms, attention, positions)
     out.backward(dout)
     return out.detach(), x.grad

@@ -1,0 +1,152 @@
+// Host side of attention and of the rotation by positions: part of slope_lib.cu, whose argument checks and launches it uses.
+#pragma once
+#include <climits>
+#include <cmath>
+
+#include "attention_kernels.cuh"
+
+namespace slope {
+// A matrix [b x heads * head_dim] of row stride `ld` as columns, heads, rows; boxes of 64 columns of a head and 128 rows, 128-byte swizzle.
+// Columns past the head and rows past the matrix read as zeros.
+static bool make_tmap_heads(CUtensorMap* tm, const void* base, int b, int heads, int head_dim, int ld) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t gdim[3] = {static_cast<cuuint64_t>(head_dim), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(b)};
+    const cuuint64_t gstride[2] = {static_cast<cuuint64_t>(head_dim) * 2, static_cast<cuuint64_t>(ld) * 2};
+    const cuuint32_t box[3] = {64, 1, kAttnRows};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return tmap_memo(tm, TmapKey{base, b, ld, heads, head_dim, 4}, [&](CUtensorMap* out) {
+        return fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), gdim, gstride, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    });
+}
+
+static bool heads_ok(int b, int heads, int kv_heads, int head_dim) {
+    return b > 0 && b <= 1 << 30 && heads > 0 && kv_heads > 0 && heads % kv_heads == 0 && head_dim > 0 && head_dim % 8 == 0 && head_dim <= 128 &&
+           static_cast<long long>(heads) * head_dim <= INT_MAX;
+}
+static bool ld_ok(int ld, int heads, int head_dim) { return ld >= heads * head_dim && ld % 8 == 0; }
+// CTAs of a launch that takes `rows` rows of a sequence each: with starts, which only the device knows, every sequence may end inside a tile.
+static long long attn_units(int b, int sequences, bool starts, int rows) {
+    if (starts) return static_cast<long long>(b) / rows + sequences;
+    return static_cast<long long>((b / sequences - 1) / rows + 1) * sequences;
+}
+static slope_status_t attn_batch(AttnShape* s, int b, int heads, int kv_heads, int head_dim, int sequences, const void* starts, const void* lengths,
+                                 int causal, int window, float scale) {
+    if (!(scale > 0.0f && scale <= FLT_MAX) || window < 0 || (window && !causal)) return SLOPE_ERR_INVALID_ARG;
+    if (!heads_ok(b, heads, kv_heads, head_dim) || sequences < 1 || (!starts && b % sequences != 0)) return SLOPE_ERR_SHAPE;
+    if (attn_units(b, sequences, starts, kAttnRows) * heads > INT_MAX) return SLOPE_ERR_SHAPE;
+    *s = AttnShape{b, heads, kv_heads, head_dim, sequences, static_cast<const int*>(starts), static_cast<const int*>(lengths), causal != 0,
+                   window < b ? window : 0, scale * kLog2e};
+    return SLOPE_OK;
+}
+template <typename Kernel, typename... Args>
+static slope_status_t launch_attn(Kernel kern, long long grid, int smem, cudaStream_t stream, const Args&... args) {
+    if (!set_smem(kern, smem)) return SLOPE_ERR_CUDA;
+    return launch_cluster_ex(kern, static_cast<int>(grid), 1, kAttnThreads, smem, /*overlap_prologue=*/true, stream, args...);
+}
+template <int HD>
+static slope_status_t attn_fwd(const AttnFwdParams& p, const CUtensorMap (&tm)[3], cudaStream_t stream) {
+    return launch_attn(attention_fwd_kernel<HD>, attn_units(p.s.b, p.s.sequences, p.s.starts, 2 * kAttnRows) * p.s.heads, AttnCfg<HD>::kSmem, stream,
+                       tm[0], tm[1], tm[2], p);
+}
+template <int HD>
+static slope_status_t attn_bwd(const AttnBwdParams& p, const AttnDeltaParams& d, const CUtensorMap (&tm)[4], cudaStream_t stream) {
+    const long long blocks = static_cast<long long>((p.s.b - 1) / 32 + 1) * ((p.s.heads + 7) / 8);
+    if (slope_status_t st = launch_cluster_ex(attention_delta_kernel<HD>, static_cast<int>(blocks), 1, 256, 0, /*overlap_prologue=*/true, stream, d)) return st;
+    const long long units = attn_units(p.s.b, p.s.sequences, p.s.starts, kAttnRows);
+    if (slope_status_t st = launch_attn(attention_bwd_kv_kernel<HD>, units * p.s.kv_heads, AttnCfg<HD>::kKvSmem, stream, tm[0], tm[1], tm[2], tm[3], p))
+        return st;
+    return launch_attn(attention_bwd_q_kernel<HD>, units * p.s.heads, AttnCfg<HD>::kSmem, stream, tm[0], tm[1], tm[2], tm[3], p);
+}
+template <int TYPE, bool PAIRS>
+static slope_status_t launch_rotary(const RotaryParams& p, int wide, cudaStream_t stream) {
+    const auto kern = wide == 8   ? rotary_kernel<TYPE, PAIRS, 8>
+                      : wide == 4 ? rotary_kernel<TYPE, PAIRS, 4>
+                      : wide == 2 ? rotary_kernel<TYPE, PAIRS, 2>
+                                  : rotary_kernel<TYPE, PAIRS, PAIRS ? 2 : 1>;
+    return launch_cluster_ex(kern, (p.b - 1) / p.tokens + 1, 1, kRotaryThreads, 0, /*overlap_prologue=*/true, stream, p);
+}
+}  // namespace slope
+
+extern "C" {
+
+slope_status_t slope_attention_fwd(const void* Q, int q_ld, const void* K, int k_ld, const void* V, int v_ld, int b, int heads, int kv_heads,
+                                   int head_dim, int sequences, const void* starts, const void* lengths, int causal, int window, float scale,
+                                   void* O, int o_ld, void* lse, void* stream_) {
+    if (!Q || !K || !V || !O) return SLOPE_ERR_INVALID_ARG;
+    AttnShape s;
+    if (slope_status_t st = attn_batch(&s, b, heads, kv_heads, head_dim, sequences, starts, lengths, causal, window, scale)) return st;
+    if (!ld_ok(q_ld, heads, head_dim) || !ld_ok(o_ld, heads, head_dim) || !ld_ok(k_ld, kv_heads, head_dim) || !ld_ok(v_ld, kv_heads, head_dim))
+        return SLOPE_ERR_SHAPE;
+    for (const void* p : {Q, K, V, starts, lengths, static_cast<const void*>(O), static_cast<const void*>(lse)})
+        if (!aligned16(p)) return SLOPE_ERR_ALIGNMENT;
+    DeviceInfo info;
+    if (slope_status_t st = check_arch(info)) return st;
+    CUtensorMap tm[3];
+    if (!make_tmap_heads(&tm[0], Q, b, heads, head_dim, q_ld) || !make_tmap_heads(&tm[1], K, b, kv_heads, head_dim, k_ld) ||
+        !make_tmap_heads(&tm[2], V, b, kv_heads, head_dim, v_ld))
+        return SLOPE_ERR_CUDA;
+    const AttnFwdParams p{s, static_cast<uint16_t*>(O), static_cast<float*>(lse), o_ld};
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    return head_dim <= 64 ? attn_fwd<64>(p, tm, stream) : attn_fwd<128>(p, tm, stream);
+}
+
+size_t slope_attention_bwd_workspace_bytes(int b, int heads, int kv_heads, int head_dim) {
+    return heads_ok(b, heads, kv_heads, head_dim) ? static_cast<size_t>(b) * heads * sizeof(float) : 0;
+}
+
+slope_status_t slope_attention_bwd(const void* dO, int do_ld, const void* Q, int q_ld, const void* K, int k_ld, const void* V, int v_ld,
+                                   const void* O, int o_ld, const void* lse, int b, int heads, int kv_heads, int head_dim, int sequences,
+                                   const void* starts, const void* lengths, int causal, int window, float scale, void* dQ, int dq_ld, void* dK,
+                                   int dk_ld, void* dV, int dv_ld, void* workspace, size_t workspace_bytes, void* stream_) {
+    if (!dO || !Q || !K || !V || !O || !lse || !dQ || !dK || !dV || !workspace) return SLOPE_ERR_INVALID_ARG;
+    AttnShape s;
+    if (slope_status_t st = attn_batch(&s, b, heads, kv_heads, head_dim, sequences, starts, lengths, causal, window, scale)) return st;
+    for (int ld : {do_ld, q_ld, o_ld, dq_ld})
+        if (!ld_ok(ld, heads, head_dim)) return SLOPE_ERR_SHAPE;
+    for (int ld : {k_ld, v_ld, dk_ld, dv_ld})
+        if (!ld_ok(ld, kv_heads, head_dim)) return SLOPE_ERR_SHAPE;
+    for (const void* p : {dO, Q, K, V, O, lse, starts, lengths, static_cast<const void*>(dQ), static_cast<const void*>(dK),
+                          static_cast<const void*>(dV), static_cast<const void*>(workspace)})
+        if (!aligned16(p)) return SLOPE_ERR_ALIGNMENT;
+    if (workspace_bytes < slope_attention_bwd_workspace_bytes(b, heads, kv_heads, head_dim)) return SLOPE_ERR_INVALID_ARG;
+    DeviceInfo info;
+    if (slope_status_t st = check_arch(info)) return st;
+    CUtensorMap tm[4];
+    if (!make_tmap_heads(&tm[0], Q, b, heads, head_dim, q_ld) || !make_tmap_heads(&tm[1], K, b, kv_heads, head_dim, k_ld) ||
+        !make_tmap_heads(&tm[2], V, b, kv_heads, head_dim, v_ld) || !make_tmap_heads(&tm[3], dO, b, heads, head_dim, do_ld))
+        return SLOPE_ERR_CUDA;
+    float* delta = static_cast<float*>(workspace);
+    const AttnBwdParams p{s,    static_cast<const float*>(lse), delta, static_cast<uint16_t*>(dQ), static_cast<uint16_t*>(dK), static_cast<uint16_t*>(dV),
+                          dq_ld, dk_ld, dv_ld, scale};
+    const AttnDeltaParams d{static_cast<const uint16_t*>(O), static_cast<const uint16_t*>(dO), o_ld, do_ld, b, heads, head_dim, delta};
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    return head_dim <= 64 ? attn_bwd<64>(p, d, tm, stream) : attn_bwd<128>(p, d, tm, stream);
+}
+
+slope_status_t slope_rotary(const void* Q, int q_ld, const void* K, int k_ld, int type, int b, int heads, int kv_heads, int head_dim, int rot_dim,
+                            int interleaved, int backward, const void* positions, const void* frequencies, float factor, void* Qr, int qr_ld,
+                            void* Kr, int kr_ld, void* stream) {
+    if (!Q || !Qr || !positions || !frequencies || !K != !Kr || !plain_type(type) || !std::isfinite(factor)) return SLOPE_ERR_INVALID_ARG;
+    if ((K && Q == Qr) != (K && K == Kr) || (Q == Qr && q_ld != qr_ld) || (K && K == Kr && k_ld != kr_ld)) return SLOPE_ERR_INVALID_ARG;
+    if (b < 1 || heads < 1 || (K && kv_heads < 1) || head_dim < 8 || head_dim % 8 != 0 || head_dim > 2 * kRotaryTable) return SLOPE_ERR_SHAPE;
+    if (rot_dim < 2 || rot_dim % 2 != 0 || rot_dim > head_dim) return SLOPE_ERR_SHAPE;
+    const auto ld_fits = [&](int ld, int n) { return ld % 8 == 0 && static_cast<long long>(n) * head_dim <= ld; };
+    if (!ld_fits(q_ld, heads) || !ld_fits(qr_ld, heads) || (K && (!ld_fits(k_ld, kv_heads) || !ld_fits(kr_ld, kv_heads)))) return SLOPE_ERR_SHAPE;
+    for (const void* p : {Q, K, positions, frequencies, static_cast<const void*>(Qr), static_cast<const void*>(Kr)})
+        if (!aligned16(p)) return SLOPE_ERR_ALIGNMENT;
+    DeviceInfo info;
+    if (slope_status_t st = check_arch(info)) return st;
+    RotaryParams p{{Q, K}, {Qr, Kr}, {q_ld, k_ld}, {qr_ld, kr_ld}, {heads, K ? kv_heads : 0}, b, head_dim, rot_dim / 2, 1, Q != Qr, factor,
+                   backward ? -1.0f : 1.0f, static_cast<const int*>(positions), static_cast<const double*>(frequencies)};
+    // an angle for every thread
+    p.tokens = std::max(1, std::min({kRotaryThreads / p.n, 64, INT_MAX / std::max(q_ld, 1) / 4, INT_MAX / std::max(k_ld, 1) / 4}));
+    // as many values at a time as the rotated part is a multiple of
+    const int unit = interleaved ? rot_dim : rot_dim / 2, wide = unit % 8 == 0 ? 8 : unit % 4 == 0 ? 4 : unit % 2 == 0 ? 2 : 1;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (type == SLOPE_F32) return interleaved ? launch_rotary<kTypeF32, true>(p, wide, s) : launch_rotary<kTypeF32, false>(p, wide, s);
+    return interleaved ? launch_rotary<kTypeBf16, true>(p, wide, s) : launch_rotary<kTypeBf16, false>(p, wide, s);
+}
+
+}  // extern "C"

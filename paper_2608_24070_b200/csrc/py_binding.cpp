@@ -28,7 +28,8 @@ namespace {
     X(slope_sparse_add) X(slope_update_sparse_matrix) X(slope_prune_nm) X(slope_double_prune_nm) X(slope_apply_mask)    \
     X(slope_dense_linear_fwd) X(slope_dense_linear_bwd_dx) X(slope_dense_linear_bwd_dw)                                 \
     X(slope_checkpoint_store) X(slope_checkpoint_load) X(slope_layer_norm_fwd) X(slope_layer_norm_bwd)                  \
-    X(slope_linear_bwd_dw_masked_q8) X(slope_linear_bwd_dw_adapter_q8) X(slope_dense_linear_bwd_dw_q8)
+    X(slope_linear_bwd_dw_masked_q8) X(slope_linear_bwd_dw_adapter_q8) X(slope_dense_linear_bwd_dw_q8) \
+    X(slope_rotary) X(slope_attention_fwd) X(slope_attention_bwd)
 
 // the library's entry points, looked up in the handle that binding.lib() loaded
 #define SLOPE_POINTER(name) decltype(&::name) p_##name = nullptr;
@@ -401,6 +402,120 @@ SLOPE_PY(slope_dense_linear_bwd_dw_q8) {
         const int64_t b = dY.size(0), d_out = dY.size(1), d_in = dW.size(1);
         return call(p_slope_dense_linear_bwd_dw_q8, checked(&dY, b, d_out, at::kBFloat16), checked_checkpoint(&Xc, b, d_in), rows(dY), cols(dY),
                     extent(d_in), checked(&dW, d_out, d_in, at::kBFloat16), ws.at, ws.bytes);
+    });
+}
+
+// A matrix whose rows may be further apart than they are long: columns of a wider one.
+struct Rows {
+    void* at;
+    int64_t rows, cols;
+    int ld;
+    at::ScalarType type;
+};
+Rows strided(const at::Tensor& t) {
+    if (!t.is_cuda() || t.dim() != 2 || (t.size(1) > 1 && t.stride(1) != 1)) {
+        PyErr_SetString(PyExc_AssertionError, "expected CUDA matrices whose rows are contiguous");
+        throw Bad{};
+    }
+    on_this_device(t);
+    // (the stride of a single row says nothing)
+    return Rows{t.data_ptr(), t.size(0), t.size(1), extent(t.size(0) > 1 ? t.stride(0) : (t.size(1) + 7) / 8 * 8), t.scalar_type()};
+}
+Rows strided(Args& a) {
+    PyObject* o = a.next();
+    if (!THPVariable_Check(o)) refuse(PyExc_TypeError, "expected a torch tensor");
+    return strided(THPVariable_Unpack(o));
+}
+Rows strided_or_none(Args& a) {
+    if (a.left > 0 && *a.at == Py_None) {
+        a.next();
+        return Rows{nullptr, 0, 0, 0, at::kBFloat16};
+    }
+    return strided(a);
+}
+void same(const Rows& a, const Rows& like) {
+    if (a.type != like.type) refuse(PyExc_TypeError, "tensor of the wrong type");
+    if (a.rows != like.rows || a.cols != like.cols) refuse(PyExc_ValueError, "tensor of the wrong shape");
+}
+int heads_of(const Rows& m, int head_dim) {
+    if (head_dim < 1 || m.cols % head_dim != 0) refuse(PyExc_ValueError, "the columns are no whole number of heads");
+    return extent(m.cols / head_dim);
+}
+SLOPE_PY(slope_rotary) {
+    return guarded(args, n, [](Args& a) {
+        const Rows Q = strided(a), K = strided_or_none(a);
+        const at::Tensor &positions = a.tensor(), &frequencies = a.tensor();
+        const int head_dim = a.integer();
+        const Rows Qr = strided(a), Kr = strided_or_none(a);
+        const float factor = a.number();
+        const int interleaved = a.integer(), backward = a.integer();
+        if (Q.type != at::kBFloat16 && Q.type != at::kFloat) refuse(PyExc_TypeError, "expected a bf16 or fp32 tensor");
+        same(Qr, Q);
+        if (!K.at != !Kr.at) refuse(PyExc_ValueError, "keys and their result belong together");
+        if (K.at) {
+            same(Kr, K);
+            if (K.type != Q.type) refuse(PyExc_TypeError, "tensor of the wrong type");
+            if (K.rows != Q.rows) refuse(PyExc_ValueError, "tensor of the wrong shape");
+        }
+        if (frequencies.dim() != 1) refuse(PyExc_ValueError, "tensor of the wrong shape");
+        void *pos = checked(&positions, 0, Q.rows, at::kInt), *freq = checked(&frequencies, 0, frequencies.size(0), at::kDouble);
+        return call(p_slope_rotary, Q.at, Q.ld, K.at, K.ld, Q.type == at::kFloat ? SLOPE_F32 : SLOPE_BF16, extent(Q.rows), heads_of(Q, head_dim),
+                    K.at ? heads_of(K, head_dim) : 0, head_dim, extent(2 * frequencies.size(0)), interleaved, backward, pos, freq, factor, Qr.at, Qr.ld,
+                    Kr.at, Kr.ld);
+    });
+}
+// What both attention calls take of a batch.
+struct Batch {
+    int sequences, causal, window;
+    void *starts, *lengths;
+    float scale;
+    explicit Batch(Args& a) {
+        sequences = a.integer();
+        const at::Tensor *s = a.tensor_or_none(), *l = a.tensor_or_none();
+        causal = a.integer();
+        window = a.integer();
+        scale = a.number();
+        starts = checked(s, 0, static_cast<int64_t>(sequences) + 1, at::kInt);
+        lengths = checked(l, 0, sequences, at::kInt);
+    }
+};
+void attention_operands(const Rows& Q, const Rows& K, const Rows& V) {
+    if (Q.type != at::kBFloat16 || K.type != at::kBFloat16) refuse(PyExc_TypeError, "tensor of the wrong type");
+    if (K.rows != Q.rows) refuse(PyExc_ValueError, "tensor of the wrong shape");
+    same(V, K);
+}
+SLOPE_PY(slope_attention_fwd) {
+    return guarded(args, n, [](Args& a) {
+        const Rows Q = strided(a), K = strided(a), V = strided(a);
+        const int head_dim = a.integer();
+        const Rows O = strided(a);
+        const at::Tensor* lse = a.tensor_or_none();
+        const Batch s(a);
+        attention_operands(Q, K, V);
+        same(O, Q);
+        const int heads = heads_of(Q, head_dim), kv_heads = heads_of(K, head_dim);
+        return call(p_slope_attention_fwd, Q.at, Q.ld, K.at, K.ld, V.at, V.ld, extent(Q.rows), heads, kv_heads, head_dim, s.sequences, s.starts, s.lengths,
+                    s.causal, s.window, s.scale, O.at, O.ld, checked(lse, heads, Q.rows, at::kFloat));
+    });
+}
+SLOPE_PY(slope_attention_bwd) {
+    return guarded(args, n, [](Args& a) {
+        const Rows dO = strided(a), Q = strided(a), K = strided(a), V = strided(a), O = strided(a);
+        const at::Tensor& lse = a.tensor();
+        const int head_dim = a.integer();
+        const Rows dQ = strided(a), dK = strided(a), dV = strided(a);
+        const Scratch ws(a.tensor_or_none());
+        const Batch s(a);
+        attention_operands(Q, K, V);
+        same(dO, Q);
+        same(O, Q);
+        same(dQ, Q);
+        same(dK, K);
+        same(dV, K);
+        const int heads = heads_of(Q, head_dim), kv_heads = heads_of(K, head_dim);
+        return call(p_slope_attention_bwd, dO.at, dO.ld, Q.at, Q.ld, K.at, K.ld, V.at, V.ld, O.at, O.ld, checked(&lse, heads, Q.rows, at::kFloat),
+                    extent(Q.rows), heads, kv_heads, head_dim, s.sequences, s.starts, s.lengths, s.causal, s.window, s.scale, dQ.at, dQ.ld, dK.at,
+                    dK.ld, dV.at, dV.ld, ws.at, ws.bytes);
     });
 }
 

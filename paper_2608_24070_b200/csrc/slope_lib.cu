@@ -1508,3 +1508,4 @@ slope_status_t slope_adapter_dl_noalloc(const void* X, const void* dT, int b, in
 }  // extern "C"
 
 #include "norm_host.cuh"
+#include "attention_host.cuh"
