@@ -41,23 +41,26 @@ static slope_status_t attn_batch(AttnShape* s, int b, int heads, int kv_heads, i
     return SLOPE_OK;
 }
 template <typename Kernel, typename... Args>
-static slope_status_t launch_attn(Kernel kern, long long grid, int smem, cudaStream_t stream, const Args&... args) {
+static slope_status_t launch_attn(Kernel kern, long long grid, int threads, int smem, cudaStream_t stream, const Args&... args) {
     if (!set_smem(kern, smem)) return SLOPE_ERR_CUDA;
-    return launch_cluster_ex(kern, static_cast<int>(grid), 1, kAttnThreads, smem, /*overlap_prologue=*/true, stream, args...);
+    return launch_cluster_ex(kern, static_cast<int>(grid), 1, threads, smem, /*overlap_prologue=*/true, stream, args...);
 }
 template <int HD>
 static slope_status_t attn_fwd(const AttnFwdParams& p, const CUtensorMap (&tm)[3], cudaStream_t stream) {
-    return launch_attn(attention_fwd_kernel<HD>, attn_units(p.s.b, p.s.sequences, p.s.starts, 2 * kAttnRows) * p.s.heads, AttnCfg<HD>::kSmem, stream,
-                       tm[0], tm[1], tm[2], p);
+    return launch_attn(attention_fwd_kernel<HD>, attn_units(p.s.b, p.s.sequences, p.s.starts, 2 * kAttnRows) * p.s.heads, kAttnThreads,
+                       AttnCfg<HD>::kSmem, stream, tm[0], tm[1], tm[2], p);
 }
 template <int HD>
 static slope_status_t attn_bwd(const AttnBwdParams& p, const AttnDeltaParams& d, const CUtensorMap (&tm)[4], cudaStream_t stream) {
     const long long blocks = static_cast<long long>((p.s.b - 1) / 32 + 1) * ((p.s.heads + 7) / 8);
     if (slope_status_t st = launch_cluster_ex(attention_delta_kernel<HD>, static_cast<int>(blocks), 1, 256, 0, /*overlap_prologue=*/true, stream, d)) return st;
     const long long units = attn_units(p.s.b, p.s.sequences, p.s.starts, kAttnRows);
-    if (slope_status_t st = launch_attn(attention_bwd_kv_kernel<HD>, units * p.s.kv_heads, AttnCfg<HD>::kKvSmem, stream, tm[0], tm[1], tm[2], tm[3], p))
+    // tiles begin on a multiple of 1 KB behind what has a fixed place
+    constexpr int kKvFixed = sizeof(AttnKvShared<AttnCfg<HD>::kStages>), kKvSmem = (2 + AttnCfg<HD>::kStages) * AttnCfg<HD>::kTile + (kKvFixed + 1023) / 1024 * 1024 - kKvFixed;
+    static_assert(kKvFixed % 16 == 0 && kKvFixed + kKvSmem <= 227 * 1024, "shared memory of the kernel of dK and dV");
+    if (slope_status_t st = launch_attn(attention_bwd_kv_kernel<HD>, units * p.s.kv_heads, kAttnThreads, kKvSmem, stream, tm[0], tm[1], tm[2], tm[3], p))
         return st;
-    return launch_attn(attention_bwd_q_kernel<HD>, units * p.s.heads, AttnCfg<HD>::kSmem, stream, tm[0], tm[1], tm[2], tm[3], p);
+    return launch_attn(attention_bwd_q_kernel<HD>, units * p.s.heads, kAttnThreads, AttnCfg<HD>::kSmem, stream, tm[0], tm[1], tm[2], tm[3], p);
 }
 template <int TYPE, bool PAIRS>
 static slope_status_t launch_rotary(const RotaryParams& p, int wide, cudaStream_t stream) {
@@ -140,8 +143,11 @@ slope_status_t slope_rotary(const void* Q, int q_ld, const void* K, int k_ld, in
     if (slope_status_t st = check_arch(info)) return st;
     RotaryParams p{{Q, K}, {Qr, Kr}, {q_ld, k_ld}, {qr_ld, kr_ld}, {heads, K ? kv_heads : 0}, b, head_dim, rot_dim / 2, 1, Q != Qr, factor,
                    backward ? -1.0f : 1.0f, static_cast<const int*>(positions), static_cast<const double*>(frequencies)};
-    // an angle for every thread
-    p.tokens = std::max(1, std::min({kRotaryThreads / p.n, 64, INT_MAX / std::max(q_ld, 1) / 4, INT_MAX / std::max(k_ld, 1) / 4}));
+    // Tokens of a block: an angle for every thread, if that leaves four blocks for every SM, or a few tasks for every thread (rotating 20 of 80 columns of
+    // 64 heads, 2039 tokens: 25 tokens a block 116 us, 3 tokens 8)
+    const long long tasks = (static_cast<long long>(heads) + p.heads[1]) * (head_dim / 8) / 2 + 1;
+    const long long most = std::min<long long>({kRotaryThreads / p.n, b / (4ll * info.sm_count), 8 * kRotaryThreads / tasks, 64});
+    p.tokens = static_cast<int>(std::max(1ll, most));
     // as many values at a time as the rotated part is a multiple of
     const int unit = interleaved ? rot_dim : rot_dim / 2, wide = unit % 8 == 0 ? 8 : unit % 4 == 0 ? 4 : unit % 2 == 0 ? 2 : 1;
     cudaStream_t s = static_cast<cudaStream_t>(stream);

@@ -50,6 +50,22 @@ __device__ __forceinline__ void tmem_st_32(uint32_t taddr, const uint32_t* v) {
         "r"(v[30]), "r"(v[31])
         : "memory");
 }
+__device__ __forceinline__ void tmem_st_16(uint32_t taddr, const uint32_t* v) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+        "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+        : "memory");
+}
+// The wait for loads from tensor memory, tied to the registers that they fill, so that nothing that uses these is moved in front of it.
+#define SLOPE_TIE8(v, i) "+r"((v)[i]), "+r"((v)[i + 1]), "+r"((v)[i + 2]), "+r"((v)[i + 3]), "+r"((v)[i + 4]), "+r"((v)[i + 5]), "+r"((v)[i + 6]), "+r"((v)[i + 7])
+__device__ __forceinline__ void tmem_ld_wait_32(uint32_t* v) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : SLOPE_TIE8(v, 0), SLOPE_TIE8(v, 8), SLOPE_TIE8(v, 16), SLOPE_TIE8(v, 24)::"memory");
+}
+// Nothing but the tie.
+__device__ __forceinline__ void tie_32(uint32_t* v) {
+    asm volatile("" : SLOPE_TIE8(v, 0), SLOPE_TIE8(v, 8), SLOPE_TIE8(v, 16), SLOPE_TIE8(v, 24)::"memory");
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
@@ -150,8 +166,19 @@ struct AttnCfg {
     static constexpr int kChunks = HD / 64, kTile = kChunks * kAttnChunk;
     static constexpr int kStages = HD == 128 ? 5 : 8;           // of the ring, beside two tiles that stay
     static constexpr int kSmem = (2 + kStages) * kTile + 1024;
-    // the kernel of dK and dV keeps 2 KB beside its tiles
-    static constexpr int kKvStages = HD == 128 ? 4 : 8, kKvSmem = (2 + kKvStages) * kTile + 1024;
+    // of the kernel of dQ: places for K, which stay until dQ has them, and for V
+    static constexpr int kKeys = HD == 128 ? 3 : 4, kValues = kStages - kKeys;
+};
+// What the kernel of dK and dV has beside its tiles.
+template <int STAGES>
+struct alignas(16) AttnKvShared {
+    uint4 minus_d[kAttnRows];             // of a tile's queries: -D / 2 as a sum of three bf16 values, zeros behind them
+    uint4 ones[8];                        // eight rows of three ones
+    float lse[kAttnRows];                 // in powers of two
+    uint64_t k_full, v_full, acc_full, s_full[2], s_read[2], dp_full[2], pairs_full[2], powers_done, d_full, full[STAGES], empty[STAGES], ragged[STAGES];
+    uint32_t tmem;
+    int abort_word;
+    AttnTile work;
 };
 template <int HD>
 __device__ __forceinline__ void attn_load(uint8_t* tile, const CUtensorMap* tm, uint64_t* bar, int head, int row) {
@@ -159,26 +186,46 @@ __device__ __forceinline__ void attn_load(uint8_t* tile, const CUtensorMap* tm, 
 #pragma unroll
     for (int c = 0; c < AttnCfg<HD>::kChunks; ++c) tma_load_3d(tile + c * kAttnChunk, tm, bar, 64 * c, head, row);
 }
-// D[128 x 128] = A B^T over the columns of a head, `steps` of 16
+// Descriptors of a tile read with its columns as the reduction, and with its rows; a step of 16 along either is a constant further on in the
+// address field.  (What the one thread computes per product it cannot issue meanwhile: with descriptors made from addresses each time, 8 products took it
+// 450 to 600 clocks, the time that they run.)
+__device__ __forceinline__ uint64_t attn_column_desc(const uint8_t* tile) { return make_smem_desc(smem_u32(tile), 16, 1024, kSwizzle128B); }
+__device__ __forceinline__ uint64_t attn_row_desc(const uint8_t* tile) { return make_smem_desc(smem_u32(tile), kAttnChunk, 1024, kSwizzle128B); }
+// D[128 x 128] (+)= A B^T over the columns of a head, `steps` of 16
 template <int HD>
-__device__ __forceinline__ void attn_mma_columns(uint32_t d, uint32_t a, uint32_t b, int steps) {
+__device__ __forceinline__ void attn_mma_columns(uint32_t d, uint64_t a, uint64_t b, int steps, bool accumulate = false) {
     constexpr uint32_t idesc = make_idesc_bf16(kAttnRows, kAttnRows, false, false, false);
+    const auto product = [&](int k) {
+        const uint32_t off = ((k >> 2) * kAttnChunk + (k & 3) * 32) >> 4;
+        umma_bf16(d, a + off, b + off, idesc, accumulate || k != 0);
+    };
+    if (steps == HD / 16) {
 #pragma unroll
-    for (int k = 0; k < HD / 16; ++k) {
-        const uint32_t off = (k >> 2) * kAttnChunk + (k & 3) * 32;
-        if (k < steps)
-            umma_bf16(d, make_smem_desc(a + off, 16, 1024, kSwizzle128B), make_smem_desc(b + off, 16, 1024, kSwizzle128B), idesc, k != 0);
+        for (int k = 0; k < HD / 16; ++k) product(k);
+    } else {
+#pragma unroll 1
+        for (int k = 0; k < steps; ++k) product(k);
     }
 }
-// D[128 x head] (+)= A B over the tile's rows, `steps` of 16; A from tensor memory: its first 64 values at `a0`, the others at `a1`
-__device__ __forceinline__ void attn_mma_rows(uint32_t d, uint32_t a0, uint32_t a1, uint32_t b, uint32_t idesc, int steps, bool accumulate) {
+// D[128 x head] (+)= A B over 64 of a tile's rows, `steps` of 16; A from tensor memory, 32 values every CHUNK columns
+template <int CHUNK = 16>
+__device__ __forceinline__ void attn_mma_rows(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, int steps, bool accumulate) {
+    const auto product = [&](int k) { umma_bf16_ts(d, a + CHUNK * (k >> 1) + 8 * (k & 1), b + k * (2048 >> 4), idesc, accumulate || k != 0); };
+    if (steps >= 4) {
 #pragma unroll
-    for (int k = 0; k < kAttnRows / 16; ++k) {
-        if (k < steps)
-            umma_bf16_ts(d, k < 4 ? a0 + 8 * k : a1 + 8 * (k - 4), make_smem_desc(b + k * 2048, kAttnChunk, 1024, kSwizzle128B), idesc,
-                         accumulate || k != 0);
+        for (int k = 0; k < 4; ++k) product(k);
+    } else {
+#pragma unroll 1
+        for (int k = 0; k < steps; ++k) product(k);
     }
 }
+// ... over all of its rows: the first 64 values of A at `a0`, the others at `a1`
+__device__ __forceinline__ void attn_mma_rows(uint32_t d, uint32_t a0, uint32_t a1, uint64_t b, uint32_t idesc, int steps, bool accumulate) {
+    attn_mma_rows(d, a0, b, idesc, steps, accumulate);
+    attn_mma_rows(d, a1, b + (64 * 128 >> 4), idesc, steps - 4, true);
+}
+// of a product whose B is [rows x head]
+__device__ __forceinline__ uint32_t attn_row_idesc(int head_dim) { return make_idesc_bf16(kAttnRows, (head_dim + 15) & ~15, false, true, false); }
 // Rows [valid, 16-multiple) of a tile to zero: they belong to other sequences or to none, and what stands there may be an infinity or a NaN,
 // which a probability of zero does not take out of a product.  Such a tile's copies complete on a barrier of its own, for one warp that zeroes the
 // rows and then completes the barrier that the tile's readers wait for.
@@ -189,18 +236,18 @@ __device__ __forceinline__ void attn_zero_rows(uint8_t* tile, int valid) {
         for (int u = lane; u < units; u += 32) *reinterpret_cast<uint4*>(tile + c * kAttnChunk + valid * 128 + u * 16) = make_uint4(0, 0, 0, 0);
     fence_proxy_async_smem();
 }
-// This warp's 32 rows of an accumulator, columns [c0, c1) of the head, times `mul`, to bf16 rows in global memory; `stage` is shared memory of
+// This warp's 32 rows of an accumulator, COLS columns of the head from `c0` on, times `mul`, to bf16 rows in global memory; `stage` is shared memory of
 // 128 rows x HD columns.  Straight from the lanes a store would touch a row per lane.
-template <int HD>
-__device__ __forceinline__ void attn_store(uint32_t t_row, int c0, int c1, float mul, uint8_t* stage, uint16_t* out, int ld, int rows, int head_dim) {
+template <int HD, int COLS>
+__device__ __forceinline__ void attn_store(uint32_t t_row, int c0, float mul, uint8_t* stage, uint16_t* out, int ld, int rows, int head_dim) {
     const int lane = threadIdx.x & 31, row0 = 32 * ((threadIdx.x >> 5) & 3);
     const uint32_t base = smem_u32(stage) + row0 * HD * 2;
-    c1 = min(c1, head_dim);
+    const int c1 = min(c0 + COLS, head_dim);
 #pragma unroll 1
     for (int c = c0; c < c1; c += 32) {
         uint32_t v[32];
         tmem_ld_32(t_row + c, v);
-        tmem_ld_wait();
+        tmem_ld_wait_32(v);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             uint32_t w[4];
@@ -210,19 +257,22 @@ __device__ __forceinline__ void attn_store(uint32_t t_row, int c0, int c1, float
         }
     }
     __syncwarp();
-    const int first = c0 >> 3, units = (c1 >> 3) - first;
-    if (units <= 0) return;
-    for (int i = lane; i < 32 * units; i += 32) {
-        const int r = i / units, u = first + i - r * units;
-        if (row0 + r < rows) {
-            const uint4 v = lds_v4(base + r * HD * 2 + (u ^ (r & 7)) * 16);
-            *reinterpret_cast<uint4*>(out + static_cast<size_t>(row0 + r) * ld + 8 * u) = v;
-        }
-    }
+    // `kUnits` lanes take 16 bytes each of a row
+    constexpr int kUnits = COLS / 8, kRows = 32 / kUnits;
+    const int u = (c0 >> 3) + lane % kUnits, r0 = lane / kUnits;
+    if (8 * u >= c1) return;
+    uint16_t* to = out + static_cast<size_t>(row0 + r0) * ld + 8 * u;
+#pragma unroll 4
+    for (int r = r0; r < min(32, rows - row0); r += kRows, to += static_cast<size_t>(kRows) * ld)
+        *reinterpret_cast<uint4*>(to) = lds_v4(base + r * HD * 2 + (u ^ (r & 7)) * 16);
 }
-// A wait whose outcome all lanes share: what follows it is done by whole warps.
+// Waits that are often over when they begin: a test takes 40 clocks, a try with a limit of its own 75.
+__device__ __forceinline__ bool attn_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+    return mbar_test(bar, parity) || mbar_wait(bar, parity, abort_flag);
+}
+// The outcome is the same for all lanes: what follows is done by whole warps.
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-    return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag));
+    return __all_sync(0xFFFFFFFFu, attn_wait(bar, parity, abort_flag));
 }
 __device__ __forceinline__ void warp_arrive(uint64_t* bar) {
     __syncwarp();
@@ -231,14 +281,48 @@ __device__ __forceinline__ void warp_arrive(uint64_t* bar) {
 
 // =====================================================================================
 // Forward.  One CTA takes 256 queries of a head as two tiles of 128, one per group of four warps, and walks the tiles of keys once:
-//   S = Q K^T (tensor memory) -> the group that owns the tile takes a row per thread: running maximum m, P = 2^(S - m), its sum l,
-//   P as bf16 over S -> O += P V (A from tensor memory).
-// While one group forms its P the tensor cores work for the other.  m follows the true maximum only where that is more than 2^8 ahead, when the
-// thread rescales O and l itself: O / l does not depend on m, P up to 2^8 has the same relative precision, and O is not touched in most
-// steps.  P is rounded to bf16 as an operand (2^-9 relative, as any operand of these products); l sums the unrounded values in fp32.
+//   S = Q K^T (tensor memory) -> the group that owns the tile takes a row per thread: P = 2^(S - m) and its sum l, m a reference for the
+//   row's maximum -> P as bf16 over S -> O += P V (A from tensor memory).
+// While one group forms its P the tensor cores work for the other; one warp issues the products of both in turn, which keeps the groups half a period
+// apart, so that each has the special-function unit for itself.  P is handed over in two halves: the first is multiplied while the second is formed.
+// m follows the true maximum only where that is more than 2^16 ahead, when the thread rescales O and l itself: O / l does not depend on m, a value up
+// to 2^16 is as exact as one up to 1 in fp32 and bf16, and O is not touched in most steps.
+// P is rounded to bf16 as an operand (2^-9 relative on average, as any operand of these products); l sums the unrounded values in fp32.
 // Warps 0-3, 4-7: queries 0-127, 128-255; warp 8: MMAs; 9: loads; 10: zeros behind the sequence's last row of V.
 // =====================================================================================
-constexpr float kAttnSlack = 8.0f;
+constexpr float kAttnSlack = 16.0f;
+// A row's 128 scores from tensor memory and their maximum.  EDGE: those outside [lo, hi) are minus infinity.  (Two instances: as a condition inside,
+// the comparisons were carried out for every tile and cost a third of what the powers of two do.)
+template <bool EDGE>
+__device__ __forceinline__ float attn_scores(uint32_t s_row, uint32_t (&v)[kAttnRows], int lo, int hi) {
+#pragma unroll
+    for (int c = 0; c < kAttnRows; c += 32) tmem_ld_32(s_row + c, v + c);
+    float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+    for (int c = 0; c < kAttnRows; c += 32) {
+        if (c == 0) tmem_ld_wait_32(v);
+        else tie_32(v + c);
+        if (EDGE) {
+#pragma unroll
+            for (int k = c; k < c + 32; ++k)
+                if (k < lo || k >= hi) v[k] = 0xFF800000u;
+        }
+#pragma unroll
+        for (int k = c; k < c + 32; k += 2) top[(k >> 1) & 3] = max3(top[(k >> 1) & 3], __uint_as_float(v[k]), __uint_as_float(v[k + 1]));
+    }
+    return fmaxf(max3(top[0], top[1], top[2]), top[3]);
+}
+// 64 scores -> 2^(v by + less) in bf16 pairs; what they were before the rounding is added to `sum`
+__device__ __forceinline__ void attn_probabilities(const uint32_t* v, uint32_t (&w)[32], float by, float less, Pair (&sum)[2]) {
+#pragma unroll
+    for (int c = 0; c < 64; c += 2) {
+        const Pair x = fma2(pair(v[c], v[c + 1]), both(by), both(less));
+        const Pair e = pair(exp2_fast(low(x)), exp2_fast(high(x)));
+        sum[(c >> 1) & 1] = add2(sum[(c >> 1) & 1], e);
+        w[c >> 1] = pack_bf16x2(low(e), high(e));
+    }
+}
+
 struct AttnFwdParams {
     AttnShape s;
     uint16_t* O;
@@ -250,7 +334,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
 attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                      const AttnFwdParams p) {
     using Cfg = AttnCfg<HD>;
-    __shared__ uint64_t q_full[2], s_full[2], p_full[2], o_full[2], full_bar[Cfg::kStages], empty_bar[Cfg::kStages], ragged_bar;
+    __shared__ uint64_t q_full[2], s_full[2], p_full[2][2], o_full[2], full_bar[Cfg::kStages], empty_bar[Cfg::kStages], ragged_bar;
     __shared__ uint32_t tmem_slot[1];
     __shared__ int abort_word;
     __shared__ AttnTile work;
@@ -265,7 +349,8 @@ attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         for (int t = 0; t < 2; ++t) {
             mbar_init(&q_full[t], 1);
             mbar_init(&s_full[t], 1);
-            mbar_init(&p_full[t], 4);
+            mbar_init(&p_full[t][0], 4);
+            mbar_init(&p_full[t][1], 4);
             mbar_init(&o_full[t], 1);
         }
         for (int i = 0; i < Cfg::kStages; ++i) { mbar_init(&full_bar[i], 1); mbar_init(&empty_bar[i], 1); }
@@ -286,7 +371,7 @@ attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
-    const uint32_t tmem = *tmem_slot;                      // S of either tile, then O of either
+    const uint32_t tmem = *tmem_slot;                      // S of either tile, then O of either; P lies over the first and third quarter of S
     const int len = work.len, first = work.first, q0 = work.tile * 2 * kAttnRows;
     const int tiles = !len ? 0 : len - q0 > kAttnRows ? 2 : 1;
     // tiles of keys [lo, hi) of the two tiles of queries and of both
@@ -306,12 +391,13 @@ attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             if (elect_one()) {
                 PipeState ps;
                 bool ok = true;
-                for (int t = 0; t < tiles; ++t) attn_load<HD>(smem + t * Cfg::kTile, &tmQ, &q_full[t], head, first + q0 + t * kAttnRows);
                 for (int j = begin; j < end && ok; ++j) {
 #pragma unroll
                     for (int v = 0; v < 2; ++v) {
-                        if (!mbar_wait(&empty_bar[ps.stage], ps.phase ^ 1u, abort_flag)) { ok = false; break; }
-                        attn_load<HD>(ring + ps.stage * Cfg::kTile, v ? &tmV : &tmK, v && j == ragged ? &ragged_bar : &full_bar[ps.stage], kv_head, first + j * kAttnRows);
+                        if (j == begin && v < tiles) attn_load<HD>(smem + v * Cfg::kTile, &tmQ, &q_full[v], head, first + q0 + v * kAttnRows);
+                        if (!attn_wait(&empty_bar[ps.stage], ps.phase ^ 1u, abort_flag)) { ok = false; break; }
+                        attn_load<HD>(ring + ps.stage * Cfg::kTile, v ? &tmV : &tmK, v && j == ragged ? &ragged_bar : &full_bar[ps.stage], kv_head,
+                                      first + j * kAttnRows);
                         ps.advance(Cfg::kStages);
                     }
                 }
@@ -319,47 +405,47 @@ attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         } else if (warp == 8) {
             if (elect_one()) {
                 const int steps = (p.s.head_dim + 15) / 16;
-                const uint32_t idesc = make_idesc_bf16(kAttnRows, 16 * steps, false, true, false);
                 PipeState ps;                             // of the next tile of the ring to be waited for
-                uint32_t p_phase[2] = {0, 0};
+                const uint32_t idesc = attn_row_idesc(p.s.head_dim);
+                const uint64_t q_desc = attn_column_desc(smem), column_desc = attn_column_desc(ring), row_desc = attn_row_desc(ring);
+                uint32_t phase[2] = {0, 0};
                 bool ok = true;
                 const auto scores = [&](int t, int stage) {
-                    attn_mma_columns<HD>(tmem + t * kAttnRows, smem_u32(smem + t * Cfg::kTile), smem_u32(ring + stage * Cfg::kTile), steps);
+                    attn_mma_columns<HD>(tmem + t * kAttnRows, q_desc + t * (Cfg::kTile >> 4), column_desc + stage * (Cfg::kTile >> 4), steps);
                     umma_commit(&s_full[t]);
                 };
-                for (int j = begin; j < end && ok; ++j) {
-                    // the first scores; behind them each step leaves those of the next
-                    if (j == begin) {
-                        if (!(ok = mbar_wait(&full_bar[ps.stage], ps.phase, abort_flag))) break;
+                // the first scores; behind them each step leaves those of the next
+                if (begin < end && (ok = attn_wait(&full_bar[ps.stage], ps.phase, abort_flag))) {
 #pragma unroll
-                        for (int t = 0; t < 2; ++t) {
-                            if (t >= tiles || !ok) continue;
-                            if (!(ok = mbar_wait(&q_full[t], 0, abort_flag))) continue;
-                            tc_fence_after_sync();
-                            if (lo[t] <= j && j < hi[t]) scores(t, ps.stage);
-                        }
-                        umma_commit(&empty_bar[ps.stage]);
-                        ps.advance(Cfg::kStages);
-                        if (!ok) break;
+                    for (int t = 0; t < 2; ++t) {
+                        if (t >= tiles || !(ok = ok && attn_wait(&q_full[t], 0, abort_flag))) continue;
+                        tc_fence_after_sync();
+                        if (lo[t] <= begin && begin < hi[t]) scores(t, ps.stage);
                     }
-                    const int v_stage = ps.stage;
-                    if (!(ok = mbar_wait(&full_bar[ps.stage], ps.phase, abort_flag))) break;
-                    const int rows = j == ragged ? last_rows : kAttnRows;
+                    umma_commit(&empty_bar[ps.stage]);
+                    ps.advance(Cfg::kStages);
+                }
+                for (int j = begin; j < end && ok; ++j) {
+                    const int rows = j == ragged ? last_rows : kAttnRows, v_stage = ps.stage;
+                    if (!(ok = attn_wait(&full_bar[ps.stage], ps.phase, abort_flag))) break;
                     ps.advance(Cfg::kStages);
                     const int k_stage = ps.stage;
                     if (j + 1 < end) {
-                        if (!(ok = mbar_wait(&full_bar[ps.stage], ps.phase, abort_flag))) break;
+                        if (!(ok = attn_wait(&full_bar[ps.stage], ps.phase, abort_flag))) break;
                         ps.advance(Cfg::kStages);
                     }
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
                         if (lo[t] <= j && j < hi[t]) {
-                            if (!(ok = ok && mbar_wait(&p_full[t], p_phase[t], abort_flag))) continue;
-                            p_phase[t] ^= 1u;
+                            const uint32_t s = tmem + t * kAttnRows, o = tmem + 2 * kAttnRows + t * HD;
+                            const uint64_t v = row_desc + v_stage * (Cfg::kTile >> 4);
+                            if (!(ok = ok && attn_wait(&p_full[t][0], phase[t], abort_flag))) continue;
                             tc_fence_after_sync();
-                            const uint32_t s = tmem + t * kAttnRows;
-                            attn_mma_rows(tmem + 2 * kAttnRows + t * HD, s, s + 32, smem_u32(ring + v_stage * Cfg::kTile), idesc, (rows + 15) / 16,
-                                          j != lo[t]);
+                            attn_mma_rows(o, s, v, idesc, (rows + 15) / 16, j != lo[t]);
+                            if (!(ok = attn_wait(&p_full[t][1], phase[t], abort_flag))) continue;
+                            tc_fence_after_sync();
+                            attn_mma_rows(o, s + 64, v + (64 * 128 >> 4), idesc, (rows + 15) / 16 - 4, true);
+                            phase[t] ^= 1u;
                             if (j + 1 == hi[t]) umma_commit(&o_full[t]);
                         }
                         if (lo[t] <= j + 1 && j + 1 < hi[t]) scores(t, k_stage);
@@ -378,81 +464,60 @@ attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         }
     } else {
         registers_up<kAttnRegsUp>();
-        const int t = group, row = threadIdx.x & 127, i = q0 + t * kAttnRows + row;       // the query's place in its sequence
+        const int t = group, row = threadIdx.x & 127, t0 = q0 + t * kAttnRows, i = t0 + row;       // the query's place in its sequence
         const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
         const uint32_t s_row = tmem + lanes + t * kAttnRows, o_row = tmem + lanes + 2 * kAttnRows + t * HD;
         float m = -INFINITY, l = 0.0f;
         uint32_t phase = 0;
         bool ok = t < tiles;
+        const float by = p.s.scale;
         const int j_lo = t ? lo[1] : lo[0], j_hi = t ? hi[1] : hi[0];
         for (int j = j_lo; j < j_hi; ++j) {
             if (!(ok = warp_wait(&s_full[t], phase, abort_flag))) break;
             phase ^= 1u;
             tc_fence_after_sync();
+            const int c0 = j * kAttnRows;
             uint32_t v[kAttnRows];
-#pragma unroll
-            for (int c = 0; c < kAttnRows; c += 32) tmem_ld_32(s_row + c, v + c);
-            tmem_ld_wait();
-            // columns [c_lo, c_hi) of the tile are seen
-            const int c0 = j * kAttnRows, t0 = q0 + t * kAttnRows;
-            if ((p.s.causal ? c0 + kAttnRows - 1 > t0 : c0 + kAttnRows > len) || (p.s.window && t0 + kAttnRows - 1 - c0 >= p.s.window)) {
-                const int c_hi = (p.s.causal ? min(i + 1, len) : len) - c0, c_lo = p.s.window ? i - p.s.window + 1 - c0 : 0;
-#pragma unroll
-                for (int c = 0; c < kAttnRows; ++c)
-                    if (c < c_lo || c >= c_hi) v[c] = 0xFF800000u;
-            }
-            float top[4];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) top[c] = __uint_as_float(v[c]);
-#pragma unroll
-            for (int c = 4; c < kAttnRows; c += 8) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    top[k] = c + 4 + k < kAttnRows ? max3(top[k], __uint_as_float(v[c + k]), __uint_as_float(v[c + 4 + k])) : fmaxf(top[k], __uint_as_float(v[c + k]));
-            }
-            const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.s.scale;
-            if (j == j_lo) {
-                m = now;
-            } else if (__any_sync(0xFFFFFFFFu, now > m + kAttnSlack)) {
-                const float next = fmaxf(m, now), by = next == m ? 1.0f : exp2_fast(m - next);
+            float now;
+            if ((p.s.causal ? c0 + kAttnRows - 1 > t0 : c0 + kAttnRows > len) || (p.s.window && t0 + kAttnRows - 1 - c0 >= p.s.window))
+                now = attn_scores<true>(s_row, v, p.s.window ? i - p.s.window + 1 - c0 : 0, (p.s.causal ? min(i + 1, len) : len) - c0) * by;
+            else
+                now = attn_scores<false>(s_row, v, 0, kAttnRows) * by;
+            if (__any_sync(0xFFFFFFFFu, now > m + kAttnSlack)) {
+                const float next = fmaxf(m, now), part = next == m ? 1.0f : exp2_fast(m - next);
                 m = next;
-                l *= by;
+                l *= part;
+                // (the last P V has completed with these scores)
 #pragma unroll 1
-                for (int c = 0; c < p.s.head_dim; c += 32) {
+                for (int c = 0; c < (j == j_lo ? 0 : p.s.head_dim); c += 32) {
                     uint32_t o[32];
                     tmem_ld_32(o_row + c, o);
-                    tmem_ld_wait();
+                    tmem_ld_wait_32(o);
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * by);
+                    for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * part);
                     tmem_st_32(o_row + c, o);
                 }
             }
-            const Pair by = both(p.s.scale), less = both(m == -INFINITY ? 0.0f : -m);
+            const float less = m == -INFINITY ? 0.0f : -m;
             Pair sum[2] = {0, 0};
 #pragma unroll
-            for (int c = 0; c < kAttnRows; c += 2) {
-                const Pair x = fma2(pair(v[c], v[c + 1]), by, less);
-                const float e0 = exp2_fast(low(x)), e1 = exp2_fast(high(x));
-                sum[(c >> 1) & 1] = add2(sum[(c >> 1) & 1], pair(e0, e1));
-                v[c >> 1] = pack_bf16x2(e0, e1);
+            for (int h = 0; h < 2; ++h) {
+                uint32_t w[32];
+                attn_probabilities(v + 64 * h, w, by, less, sum);
+                tmem_st_32(s_row + 64 * h, w);
+                tmem_st_wait();
+                tc_fence_before_sync();
+                warp_arrive(&p_full[t][h]);
             }
-            tmem_st_32(s_row, v);
-            tmem_st_32(s_row + 32, v + 32);
             const Pair all = add2(sum[0], sum[1]);
             l += low(all) + high(all);
-            tmem_st_wait();
-            tc_fence_before_sync();
-            warp_arrive(&p_full[t]);
         }
         if (ok && (ok = warp_wait(&o_full[t], 0, abort_flag))) {
             tc_fence_after_sync();
-            const size_t at = static_cast<size_t>(first) + q0 + t * kAttnRows;
+            const size_t at = static_cast<size_t>(first) + t0;
             if (p.lse && i < len) p.lse[static_cast<size_t>(head) * p.s.b + at + row] = m * kLn2 + logf(l);
             // (a row that has seen none but infinitely small scores: 0 / 0)
-            const float inv = 1.0f / l;
-            // every lane's own row: `mul` differs between lanes
-            attn_store<HD>(o_row, 0, HD, inv, smem + t * Cfg::kTile, p.O + at * p.o_ld + head * p.s.head_dim, p.o_ld, len - q0 - t * kAttnRows,
-                           p.s.head_dim);
+            attn_store<HD, HD>(o_row, 0, 1.0f / l, smem + t * Cfg::kTile, p.O + at * p.o_ld + head * p.s.head_dim, p.o_ld, len - t0, p.s.head_dim);
         }
         tc_fence_before_sync();
     }
@@ -513,22 +578,77 @@ struct AttnBwdParams {
     float grad_scale;                     // the products' factor itself
 };
 
+// A key's 128 scores -> 2^(v by - lse): lse belongs to the query, the column, and lies in shared memory ...  EDGE: those outside [lo, hi) are 0 (two
+// instances, as in the forward pass)
+template <bool EDGE>
+__device__ __forceinline__ void attn_column_powers(uint32_t (&v)[kAttnRows], float by, uint32_t lse, int lo, int hi) {
+#pragma unroll
+    for (int c = 0; c < kAttnRows; c += 4) {
+        const float4 e = ld_shared_v4(lse + 4 * c);
+        const Pair x0 = fma2(pair(v[c], v[c + 1]), both(by), pair(-e.x, -e.y)), x1 = fma2(pair(v[c + 2], v[c + 3]), both(by), pair(-e.z, -e.w));
+        v[c] = __float_as_uint(exp2_fast(low(x0)));
+        v[c + 1] = __float_as_uint(exp2_fast(high(x0)));
+        v[c + 2] = __float_as_uint(exp2_fast(low(x1)));
+        v[c + 3] = __float_as_uint(exp2_fast(high(x1)));
+    }
+    if (EDGE) {
+#pragma unroll
+        for (int c = 0; c < kAttnRows; ++c)
+            if (c < lo || c >= hi) v[c] = 0u;
+    }
+}
+// ... and, with dP - D from tensor memory, to bf16 pairs: 32 values of P and behind them 32 of dS = P (dP - D) at a time, in the place of dP; the
+// barriers say that either half is there.
+template <bool EDGE>
+__device__ __forceinline__ void attn_column_pairs(uint32_t dp_row, uint32_t (&v)[kAttnRows], uint64_t (&half_full)[2], int lo, int hi) {
+    uint32_t g[32];
+    tmem_ld_32(dp_row, g);
+#pragma unroll
+    for (int c = 0; c < kAttnRows; c += 32) {
+        tmem_ld_wait_32(g);
+#pragma unroll
+        for (int k = 0; k < 32; k += 2) {
+            const Pair p = pair(v[c + k], v[c + k + 1]), y = mul2(p, pair(g[k], g[k + 1]));
+            v[c + (k >> 1)] = pack_bf16x2(low(p), high(p));       // (in the registers that they came in)
+            g[k >> 1] = pack_bf16x2(low(y), high(y));
+        }
+        if (EDGE) {                                         // (zero times what a row of no sequence holds)
+#pragma unroll
+            for (int k = 0; k < 32; ++k)
+                if (c + k < lo || c + k >= hi) g[k >> 1] &= k & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+        }
+        tmem_st_16(dp_row + c, v + c);
+        tmem_st_16(dp_row + c + 16, g);
+        if (c + 32 < kAttnRows) tmem_ld_32(dp_row + c + 32, g);
+        if (c & 32) {
+            tmem_st_wait();
+            tc_fence_before_sync();
+            warp_arrive(&half_full[c >> 6]);
+        }
+    }
+}
+// x as a sum of three bf16 values, exact to 2^-24 of it, in the first three eighths of a row of 16
+__device__ __forceinline__ uint4 attn_split(float x) {
+    const float h = __uint_as_float(pack_bf16x2(0.0f, x) & 0xFFFF0000u), m = __uint_as_float(pack_bf16x2(0.0f, x - h) & 0xFFFF0000u);
+    return make_uint4(pack_bf16x2(h, m), pack_bf16x2(x - h - m, 0.0f), 0u, 0u);
+}
+
 // dK and dV of 128 keys.  Keys lie on the lanes: S^T = K Q^T, dP^T = V dO^T, so that P^T and dS^T are where the next products
-// want them as A.  Both groups work on every tile, 64 queries each; what belongs to a query (lse, D) comes from shared memory.
-// The tensor cores' order is dV(i), S(i + 1), dK(i), dP(i + 1): P(i + 1) is formed beside dK(i) and dP(i + 1), dS(i) beside dV(i) and S(i + 1).
-// Warp 8: MMAs; 9: loads; 10: lse and D, zeros behind the sequence's last row.
+// want them as A.  The groups take the tiles of queries in turn, a key per thread.  What belongs to a query: lse comes from shared memory; -D is one
+// more step of 16 of the product dP^T, of rows of three ones and rows with -D / 2 in three parts (read twice: a step has two eighths), since the
+// products leave other reads of shared memory little room (16 of them per 64 values of dS: 1300 of 3700 clocks a tile).
+// A thread reads its scores at once, so that the next tile's are formed, and keeps P in registers until dP is there; P and dS then take the
+// place of dP, 32 queries at a time.  So while one group has dP and the products dV, dK and the next dP run, the other has its powers of two.
+// What bounds it is the way dP - dS - dV, dK - next dP, 2000 of whose clocks at 128 columns are the products' (2048 with S).
+// Warp 11: the MMAs of S; 8: the others; 9: loads; 10: lse and D, zeros behind the sequence's last row.
 template <int HD>
 __global__ void __launch_bounds__(kAttnThreads, 1)
 attention_bwd_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                         const __grid_constant__ CUtensorMap tmdO, const AttnBwdParams p) {
     using Cfg = AttnCfg<HD>;
-    __shared__ uint64_t k_full, v_full, s_full, dp_full, p_ready, ds_ready, acc_full, vec_full[2], vec_empty[2];
-    __shared__ uint64_t full_bar[Cfg::kKvStages], empty_bar[Cfg::kKvStages], ragged_bar[Cfg::kKvStages];
-    __shared__ __align__(16) float vec[2][2][kAttnRows];       // lse (in powers of two) and D of a tile's queries
-    __shared__ uint32_t tmem_slot[1];
-    __shared__ int abort_word;
-    __shared__ AttnTile work;
-    volatile int* abort_flag = &abort_word;
+    // (one array, whose size the host knows: beside seven tiles of 128 columns there are 3 KB)
+    __shared__ AttnKvShared<Cfg::kStages> sh;
+    volatile int* abort_flag = &sh.abort_word;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t *sK = smem, *sV = smem + Cfg::kTile, *ring = smem + 2 * Cfg::kTile;
@@ -536,32 +656,39 @@ attention_bwd_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
 
     griddep_launch_dependents();
     if (threadIdx.x == 0) {
-        for (uint64_t* bar : {&k_full, &v_full, &s_full, &dp_full, &acc_full}) mbar_init(bar, 1);
-        mbar_init(&p_ready, 8);
-        mbar_init(&ds_ready, 8);
-        for (int i = 0; i < 2; ++i) { mbar_init(&vec_full[i], 1); mbar_init(&vec_empty[i], 8); }
-        for (int i = 0; i < Cfg::kKvStages; ++i) { mbar_init(&full_bar[i], 1); mbar_init(&empty_bar[i], 1); mbar_init(&ragged_bar[i], 1); }
+        for (uint64_t* bar : {&sh.k_full, &sh.v_full, &sh.acc_full, &sh.d_full, &sh.dp_full[0], &sh.dp_full[1]}) mbar_init(bar, 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&sh.s_full[i], 2);                    // the scores, and what belongs to their queries
+            mbar_init(&sh.s_read[i], 4);
+            mbar_init(&sh.pairs_full[i], 4);
+        }
+        mbar_init(&sh.powers_done, 4);
+        for (int i = 0; i < Cfg::kStages; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); mbar_init(&sh.ragged[i], 1); }
         *abort_flag = 0;
         fence_mbar_init();
     }
+    if (threadIdx.x >= 32 && threadIdx.x < 40) {
+        sh.ones[threadIdx.x - 32] = make_uint4(0x3F803F80u, 0x00003F80u, 0u, 0u);
+        fence_proxy_async_smem();
+    }
     if (warp == 8) {
-        tmem_alloc(tmem_slot, 512);
+        tmem_alloc(&sh.tmem, 512);
         tmem_relinquish();
     }
     griddep_wait();
     const int kv_head = blockIdx.x % p.s.kv_heads, share = p.s.heads / p.s.kv_heads;
     if (warp == 0) {
         const AttnTile t = attn_locate(p.s, blockIdx.x / p.s.kv_heads, kAttnRows, false);
-        if (lane == 0) work = t;
+        if (lane == 0) sh.work = t;
     }
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
-    const uint32_t tmem = *tmem_slot, t_s = tmem, t_dp = tmem + kAttnRows, t_dv = tmem + 2 * kAttnRows, t_dk = t_dv + HD;
-    const int len = work.len, first = work.first, k0 = work.tile * kAttnRows;
-    const int lo = attn_first_query_tile(p.s, k0), per_head = len ? attn_end_query_tile(p.s, k0, len) - lo : 0, items = per_head * share;
+    const uint32_t tmem = sh.tmem, t_s = tmem, t_dp = tmem + kAttnRows, t_dv = tmem + 2 * kAttnRows, t_dk = t_dv + HD;
+    const int len = sh.work.len, first = sh.work.first, k0 = sh.work.tile * kAttnRows;
+    // an item: a tile of queries of one of the heads that share the key head
+    const int lo = attn_first_query_tile(p.s, k0), hi = len ? attn_end_query_tile(p.s, k0, len) : lo, items = (hi - lo) * share;
     const int last = (len - 1) / kAttnRows, last_rows = len - last * kAttnRows;
-    const auto tile_of = [&](int it) { return lo + it % per_head; };
     const auto rows_of = [&](int tile) { return tile == last ? last_rows : kAttnRows; };
 
     if (group == 2) {
@@ -570,167 +697,150 @@ attention_bwd_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
             if (items && elect_one()) {
                 PipeState ps;
                 bool ok = true;
-                attn_load<HD>(sK, &tmK, &k_full, kv_head, first + k0);
-                for (int it = 0; it < items && ok; ++it) {
-                    const int head = kv_head * share + it / per_head, row = first + tile_of(it) * kAttnRows;
-                    uint64_t* bars = rows_of(tile_of(it)) < kAttnRows ? ragged_bar : full_bar;
+                attn_load<HD>(sK, &tmK, &sh.k_full, kv_head, first + k0);
+                for (int it = 0, tile = lo, head = kv_head * share; it < items && ok; ++it) {
+                    uint64_t* bars = rows_of(tile) < kAttnRows ? sh.ragged : sh.full;
 #pragma unroll
                     for (int g = 0; g < 2; ++g) {
-                        if (!mbar_wait(&empty_bar[ps.stage], ps.phase ^ 1u, abort_flag)) { ok = false; break; }
-                        attn_load<HD>(ring + ps.stage * Cfg::kTile, g ? &tmdO : &tmQ, &bars[ps.stage], head, row);
-                        ps.advance(Cfg::kKvStages);
-                        if (it == 0 && g == 0) attn_load<HD>(sV, &tmV, &v_full, kv_head, first + k0);
+                        if (!attn_wait(&sh.empty[ps.stage], ps.phase ^ 1u, abort_flag)) { ok = false; break; }
+                        attn_load<HD>(ring + ps.stage * Cfg::kTile, g ? &tmdO : &tmQ, &bars[ps.stage], head, first + tile * kAttnRows);
+                        ps.advance(Cfg::kStages);
+                        if (it == 0 && g == 0) attn_load<HD>(sV, &tmV, &sh.v_full, kv_head, first + k0);
                     }
+                    if (++tile == hi) { tile = lo; ++head; }
+                }
+            }
+        } else if (warp == 11) {
+            // the scores, by a warp of its own: what they wait for does not hold the other products up
+            if (items && elect_one()) {
+                const int steps = (p.s.head_dim + 15) / 16;
+                const uint64_t k_desc = attn_column_desc(sK), column_desc = attn_column_desc(ring);
+                PipeState ps;
+                bool ok = attn_wait(&sh.k_full, 0, abort_flag);
+                for (int it = 0; it < items && ok; ++it) {
+                    if (!(ok = attn_wait(&sh.full[ps.stage], ps.phase, abort_flag) &&
+                               (it == 0 || attn_wait(&sh.s_read[(it - 1) & 1], ((it - 1) >> 1) & 1, abort_flag))))
+                        break;
+                    tc_fence_after_sync();
+                    attn_mma_columns<HD>(t_s, k_desc, column_desc + ps.stage * (Cfg::kTile >> 4), steps);
+                    umma_commit(&sh.s_full[it & 1]);
+                    ps.advance(Cfg::kStages);
+                    ps.advance(Cfg::kStages);
                 }
             }
         } else if (warp == 8) {
             if (items && elect_one()) {
                 const int steps = (p.s.head_dim + 15) / 16;
-                const uint32_t idesc = make_idesc_bf16(kAttnRows, 16 * steps, false, true, false);
-                PipeState ps;
-                int q_stage = 0, o_stage = 0, q_next = 0, o_next = 0;
-                bool ok = true;
-                const auto ready = [&](int& stage) {
-                    stage = ps.stage;
-                    const bool got = mbar_wait(&full_bar[ps.stage], ps.phase, abort_flag);
-                    ps.advance(Cfg::kKvStages);
-                    return got;
+                const uint32_t idesc = attn_row_idesc(p.s.head_dim);
+                const uint64_t v_desc = attn_column_desc(sV), column_desc = attn_column_desc(ring), row_desc = attn_row_desc(ring);
+                // rows of eight values without a swizzle, the same eight for both eighths of the step; the same eight rows of ones throughout
+                const uint64_t ones_desc = make_smem_desc(smem_u32(sh.ones), 0, 0, kSwizzleNone), d_desc = make_smem_desc(smem_u32(sh.minus_d), 0, 128, kSwizzleNone);
+                PipeState qs, os;                         // places of this item's Q and dO
+                os.advance(Cfg::kStages);
+                // (behind `d_full` dO is there, too)
+                const auto products = [&](int it) {
+                    if (!attn_wait(&sh.d_full, it & 1, abort_flag)) return false;
+                    tc_fence_after_sync();
+                    umma_bf16(t_dp, ones_desc, d_desc, make_idesc_bf16(kAttnRows, kAttnRows, false, false, false), 0);
+                    attn_mma_columns<HD>(t_dp, v_desc, column_desc + os.stage * (Cfg::kTile >> 4), steps, true);
+                    umma_commit(&sh.dp_full[it & 1]);
+                    return true;
                 };
-                const auto at = [&](int stage) { return smem_u32(ring + stage * Cfg::kTile); };
-                ok = mbar_wait(&k_full, 0, abort_flag) && ready(q_stage);
-                if (ok) {
-                    tc_fence_after_sync();
-                    attn_mma_columns<HD>(t_s, smem_u32(sK), at(q_stage), steps);
-                    umma_commit(&s_full);
-                    ok = mbar_wait(&v_full, 0, abort_flag) && ready(o_stage);
-                }
-                if (ok) {
-                    tc_fence_after_sync();
-                    attn_mma_columns<HD>(t_dp, smem_u32(sV), at(o_stage), steps);
-                    umma_commit(&dp_full);
-                }
-                for (int it = 0; it < items && ok; ++it) {
-                    const int row_steps = (rows_of(tile_of(it)) + 15) / 16;
-                    if (!(ok = mbar_wait(&p_ready, it & 1, abort_flag))) break;
-                    tc_fence_after_sync();
-                    attn_mma_rows(t_dv, t_s, t_s + 64, at(o_stage), idesc, row_steps, it != 0);
-                    umma_commit(&empty_bar[o_stage]);
-                    if (it + 1 < items) {
-                        if (!(ok = ready(q_next))) break;
+                bool ok = attn_wait(&sh.v_full, 0, abort_flag) && products(0);
+                for (int it = 0, tile = lo; it < items && ok; ++it) {
+                    const int row_steps = (rows_of(tile) + 15) / 16;
+                    if (++tile == hi) tile = lo;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if (!(ok = ok && attn_wait(&sh.pairs_full[h], it & 1, abort_flag))) continue;
                         tc_fence_after_sync();
-                        attn_mma_columns<HD>(t_s, smem_u32(sK), at(q_next), steps);
-                        umma_commit(&s_full);
+                        const uint32_t a = t_dp + 64 * h, b = h * (64 * 128 >> 4);
+                        attn_mma_rows<32>(t_dv, a, row_desc + os.stage * (Cfg::kTile >> 4) + b, idesc, row_steps - 4 * h, it != 0 || h);
+                        attn_mma_rows<32>(t_dk, a + 16, row_desc + qs.stage * (Cfg::kTile >> 4) + b, idesc, row_steps - 4 * h, it != 0 || h);
                     }
-                    if (!(ok = mbar_wait(&ds_ready, it & 1, abort_flag))) break;
-                    tc_fence_after_sync();
-                    attn_mma_rows(t_dk, t_dp, t_dp + 64, at(q_stage), idesc, row_steps, it != 0);
-                    umma_commit(it + 1 < items ? &empty_bar[q_stage] : &acc_full);
-                    if (it + 1 < items) {
-                        if (!(ok = ready(o_next))) break;
-                        tc_fence_after_sync();
-                        attn_mma_columns<HD>(t_dp, smem_u32(sV), at(o_next), steps);
-                        umma_commit(&dp_full);
-                    }
-                    q_stage = q_next;
-                    o_stage = o_next;
+                    if (!ok) break;
+                    umma_commit(&sh.empty[qs.stage]);
+                    umma_commit(&sh.empty[os.stage]);
+                    for (int g = 0; g < 2; ++g) { qs.advance(Cfg::kStages); os.advance(Cfg::kStages); }
+                    if (it + 1 < items) ok = products(it + 1);
+                    else umma_commit(&sh.acc_full);
                 }
             }
         } else if (warp == 10) {
             uint32_t phases = 0;                             // of the stages' ragged barriers
-            for (int it = 0; it < items; ++it) {
-                const int head = kv_head * share + it / per_head, tile = tile_of(it), rows = rows_of(tile), slot = it & 1;
+            for (int it = 0, tile = lo, head = kv_head * share; it < items; ++it) {
+                const int rows = rows_of(tile);
                 const size_t at = static_cast<size_t>(head) * p.s.b + first + tile * kAttnRows;
-                if (it > 1 && !warp_wait(&vec_empty[slot], ((it >> 1) & 1) ^ 1u, abort_flag)) break;
+                uint32_t e[4], d[4];
 #pragma unroll
-                for (int i = lane; i < kAttnRows; i += 32) {
-                    vec[slot][0][i] = i < rows ? __uint_as_float(ld_u32(p.lse + at + i)) * kLog2e : 0.0f;
-                    vec[slot][1][i] = i < rows ? __uint_as_float(ld_u32(p.delta + at + i)) : 0.0f;
+                for (int k = 0; k < 4; ++k) {
+                    const bool in = lane + 32 * k < rows;
+                    e[k] = in ? ld_u32(p.lse + at + lane + 32 * k) : 0u;
+                    d[k] = in ? ld_u32(p.delta + at + lane + 32 * k) : 0u;
                 }
-                warp_arrive(&vec_full[slot]);
                 if (rows < kAttnRows) {
                     bool ok = true;
                     for (int g = 0; g < 2 && ok; ++g) {
-                        const int stage = (2 * it + g) % Cfg::kKvStages;
-                        if (!(ok = warp_wait(&ragged_bar[stage], (phases >> stage) & 1, abort_flag))) break;
+                        const int stage = (2 * it + g) % Cfg::kStages;
+                        if (!(ok = warp_wait(&sh.ragged[stage], (phases >> stage) & 1, abort_flag))) break;
                         phases ^= 1u << stage;
                         attn_zero_rows<HD>(ring + stage * Cfg::kTile, rows);
-                        warp_arrive(&full_bar[stage]);
+                        warp_arrive(&sh.full[stage]);
                     }
                     if (!ok) break;
                 }
+                // the last tile's powers of two are done, and its dP
+                if (it && !warp_wait(&sh.powers_done, (it - 1) & 1, abort_flag)) break;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) sh.lse[lane + 32 * k] = __uint_as_float(e[k]) * kLog2e;
+                warp_arrive(&sh.s_full[it & 1]);
+                if (it && !warp_wait(&sh.dp_full[(it - 1) & 1], ((it - 1) >> 1) & 1, abort_flag)) break;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) sh.minus_d[lane + 32 * k] = attn_split(-0.5f * __uint_as_float(d[k]));
+                fence_proxy_async_smem();
+                if (!warp_wait(&sh.full[(2 * it + 1) % Cfg::kStages], ((2 * it + 1) / Cfg::kStages) & 1, abort_flag)) break;
+                warp_arrive(&sh.d_full);
+                if (++tile == hi) { tile = lo; ++head; }
             }
         }
     } else {
         registers_up<kAttnRegsUp>();
         const int key = k0 + (threadIdx.x & 127);
-        const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16, half = 64 * group;
-        const uint32_t s_row = t_s + lanes + half, dp_row = t_dp + lanes + half;
+        const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+        const uint32_t s_row = t_s + lanes, dp_row = t_dp + lanes;
         bool ok = items > 0;
-        for (int it = 0; it < items; ++it) {
-            const int q0 = tile_of(it) * kAttnRows, slot = it & 1;
+        for (int it = group, tile = lo + group; it < items; it += 2, tile += 2) {
+            while (tile >= hi) tile -= hi - lo;
+            const int q0 = tile * kAttnRows;
+            const uint32_t phase = (it >> 1) & 1;
             const bool edge = (p.s.causal && q0 == k0) || q0 + kAttnRows > len || (p.s.window && q0 + kAttnRows - 1 - k0 >= p.s.window);
-            // queries [c_lo, c_hi) of this group's 64 see the key
-            const int c_lo = p.s.causal ? key - q0 - static_cast<int>(half) : 0;
-            const int c_hi = min(len, p.s.window ? min(key, len) + p.s.window : len) - q0 - static_cast<int>(half);
-            if (!(ok = warp_wait(&vec_full[slot], (it >> 1) & 1, abort_flag) && warp_wait(&s_full, it & 1, abort_flag))) break;
+            // queries [c_lo, c_hi) of the tile's see the key
+            const int c_lo = p.s.causal ? key - q0 : 0, c_hi = min(len, p.s.window ? min(key, len) + p.s.window : len) - q0;
+            if (!(ok = warp_wait(&sh.s_full[group], phase, abort_flag))) break;
             tc_fence_after_sync();
-            uint32_t v[64], w[32];
-            tmem_ld_32(s_row, v);
-            tmem_ld_32(s_row + 32, v + 32);
-            tmem_ld_wait();
-            const uint32_t vec_lse = smem_u32(&vec[slot][0][half]), vec_delta = smem_u32(&vec[slot][1][half]);
-            const Pair by = both(p.s.scale);
+            uint32_t v[kAttnRows];
 #pragma unroll
-            for (int c = 0; c < 64; c += 4) {
-                const float4 e = ld_shared_v4(vec_lse + 4 * c);
-                const Pair x0 = fma2(pair(v[c], v[c + 1]), by, pair(-e.x, -e.y)), x1 = fma2(pair(v[c + 2], v[c + 3]), by, pair(-e.z, -e.w));
-                v[c] = __float_as_uint(exp2_fast(low(x0)));
-                v[c + 1] = __float_as_uint(exp2_fast(high(x0)));
-                v[c + 2] = __float_as_uint(exp2_fast(low(x1)));
-                v[c + 3] = __float_as_uint(exp2_fast(high(x1)));
-            }
-            if (edge) {
-#pragma unroll
-                for (int c = 0; c < 64; ++c)
-                    if (c < c_lo || c >= c_hi) v[c] = 0u;
-            }
-#pragma unroll
-            for (int c = 0; c < 64; c += 2) w[c >> 1] = pack_bf16x2(__uint_as_float(v[c]), __uint_as_float(v[c + 1]));
-            tmem_st_32(s_row, w);
-            tmem_st_wait();
+            for (int c = 0; c < kAttnRows; c += 32) tmem_ld_32(s_row + c, v + c);
+            tmem_ld_wait_32(v);
+            tie_32(v + 32);
+            tie_32(v + 64);
+            tie_32(v + 96);
             tc_fence_before_sync();
-            warp_arrive(&p_ready);
-            if (!(ok = warp_wait(&dp_full, it & 1, abort_flag))) break;
+            warp_arrive(&sh.s_read[group]);
+            if (edge) attn_column_powers<true>(v, p.s.scale, smem_u32(sh.lse), c_lo, c_hi);
+            else attn_column_powers<false>(v, p.s.scale, smem_u32(sh.lse), 0, kAttnRows);
+            warp_arrive(&sh.powers_done);
+            if (!(ok = warp_wait(&sh.dp_full[group], phase, abort_flag))) break;
             tc_fence_after_sync();
-            uint32_t g[64];
-            tmem_ld_32(dp_row, g);
-            tmem_ld_32(dp_row + 32, g + 32);
-            tmem_ld_wait();
-#pragma unroll
-            for (int c = 0; c < 64; c += 4) {
-                const float4 d = ld_shared_v4(vec_delta + 4 * c);
-                const Pair y0 = mul2(pair(v[c], v[c + 1]), add2(pair(g[c], g[c + 1]), pair(-d.x, -d.y)));
-                const Pair y1 = mul2(pair(v[c + 2], v[c + 3]), add2(pair(g[c + 2], g[c + 3]), pair(-d.z, -d.w)));
-                w[c >> 1] = pack_bf16x2(low(y0), high(y0));
-                w[(c >> 1) + 1] = pack_bf16x2(low(y1), high(y1));
-            }
-            if (edge) {                                     // (zero times what a row of no sequence holds)
-#pragma unroll
-                for (int c = 0; c < 64; ++c)
-                    if (c < c_lo || c >= c_hi) w[c >> 1] &= c & 1 ? 0x0000FFFFu : 0xFFFF0000u;
-            }
-            tmem_st_32(dp_row, w);
-            tmem_st_wait();
-            tc_fence_before_sync();
-            warp_arrive(&ds_ready);
-            warp_arrive(&vec_empty[slot]);
+            if (edge) attn_column_pairs<true>(dp_row, v, sh.pairs_full, c_lo, c_hi);
+            else attn_column_pairs<false>(dp_row, v, sh.pairs_full, 0, kAttnRows);
         }
-        if (ok && warp_wait(&acc_full, 0, abort_flag)) {
+        if (ok && warp_wait(&sh.acc_full, 0, abort_flag)) {
             tc_fence_after_sync();
             const size_t row = static_cast<size_t>(first) + k0;
             uint16_t* out = group ? p.dK + row * p.dk_ld : p.dV + row * p.dv_ld;
-            attn_store<HD>((group ? t_dk : t_dv) + lanes, 0, HD, group ? p.grad_scale : 1.0f, group ? sK : sV, out + kv_head * p.s.head_dim,
-                           group ? p.dk_ld : p.dv_ld, len - k0, p.s.head_dim);
+            attn_store<HD, HD>((group ? t_dk : t_dv) + lanes, 0, group ? p.grad_scale : 1.0f, group ? sK : sV, out + kv_head * p.s.head_dim,
+                               group ? p.dk_ld : p.dv_ld, len - k0, p.s.head_dim);
         }
         tc_fence_before_sync();
     }
@@ -742,29 +852,75 @@ attention_bwd_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
     }
 }
 
-// dQ of 128 queries, which lie on the lanes; both groups work on every tile of keys, 64 keys each.  S is formed a tile ahead in the other of
-// two places; dS takes the place of S.
+// A row's 128 scores from tensor memory -> 2^(v by - lse); EDGE: those outside [lo, hi) are 0
+template <bool EDGE>
+__device__ __forceinline__ void attn_row_powers(uint32_t s_row, uint32_t (&v)[kAttnRows], float by, float lse, int lo, int hi) {
+#pragma unroll
+    for (int c = 0; c < kAttnRows; c += 32) tmem_ld_32(s_row + c, v + c);
+#pragma unroll
+    for (int c = 0; c < kAttnRows; c += 32) {
+        if (c == 0) tmem_ld_wait_32(v);
+        else tie_32(v + c);
+#pragma unroll
+        for (int k = c; k < c + 32; k += 2) {
+            const Pair x = fma2(pair(v[k], v[k + 1]), both(by), both(-lse));
+            v[k] = !EDGE || (k >= lo && k < hi) ? __float_as_uint(exp2_fast(low(x))) : 0u;
+            v[k + 1] = !EDGE || (k + 1 >= lo && k + 1 < hi) ? __float_as_uint(exp2_fast(high(x))) : 0u;
+        }
+    }
+}
+// ... and, with dP from tensor memory, to dS = P (dP - D) in bf16 pairs; the barrier says that dP has been read
+template <bool EDGE>
+__device__ __forceinline__ void attn_row_gradients(uint32_t dp_row, uint32_t (&v)[kAttnRows], float d, uint64_t* dp_read, int lo, int hi) {
+    uint32_t g[2][32];
+    tmem_ld_32(dp_row, g[0]);
+#pragma unroll
+    for (int c = 0; c < kAttnRows; c += 32) {
+        uint32_t(&now)[32] = g[(c >> 5) & 1];
+        tmem_ld_wait_32(now);
+        if (c + 32 < kAttnRows) {
+            tmem_ld_32(dp_row + c + 32, g[((c >> 5) + 1) & 1]);
+        } else {
+            tc_fence_before_sync();
+            warp_arrive(dp_read);
+        }
+#pragma unroll
+        for (int k = 0; k < 32; k += 2) {
+            const Pair y = mul2(pair(v[c + k], v[c + k + 1]), add2(pair(now[k], now[k + 1]), both(-d)));
+            v[(c + k) >> 1] = pack_bf16x2(low(y), high(y));
+        }
+        if (EDGE) {                                         // (zero times what a row of no sequence holds)
+#pragma unroll
+            for (int k = c; k < c + 32; ++k)
+                if (k < lo || k >= hi) v[k >> 1] &= k & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+        }
+    }
+}
+// dQ of 128 queries, which lie on the lanes.  The groups take the tiles of keys in turn, a row per thread: while one forms its powers of two the other has
+// its dS.  S has a place for either group and is formed two tiles ahead; dS takes the place of S; dP is read as soon as it is there, so that the
+// next one is formed beside dS.  (Both groups on every tile, 64 keys each: 2400 clocks a tile.)
 template <int HD>
 __global__ void __launch_bounds__(kAttnThreads, 1)
 attention_bwd_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                        const __grid_constant__ CUtensorMap tmdO, const AttnBwdParams p) {
     using Cfg = AttnCfg<HD>;
-    __shared__ uint64_t q_full, do_full, s_full[2], dp_full, ds_ready, acc_full, ragged_bar;
-    __shared__ uint64_t full_bar[Cfg::kStages], empty_bar[Cfg::kStages];
+    __shared__ uint64_t q_full, do_full, s_full[2], dp_full[2], dp_read[2], ds_ready[2], acc_full, ragged_bar;
+    __shared__ uint64_t k_full[Cfg::kKeys], k_empty[Cfg::kKeys], v_full[Cfg::kValues], v_empty[Cfg::kValues];
     __shared__ uint32_t tmem_slot[1];
     __shared__ int abort_word;
     __shared__ AttnTile work;
     volatile int* abort_flag = &abort_word;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    uint8_t *sQ = smem, *sdO = smem + Cfg::kTile, *ring = smem + 2 * Cfg::kTile;
+    uint8_t *sQ = smem, *sdO = smem + Cfg::kTile, *keys = smem + 2 * Cfg::kTile, *values = keys + Cfg::kKeys * Cfg::kTile;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = threadIdx.x >> 7;
 
     griddep_launch_dependents();
     if (threadIdx.x == 0) {
-        for (uint64_t* bar : {&q_full, &do_full, &s_full[0], &s_full[1], &dp_full, &acc_full, &ragged_bar}) mbar_init(bar, 1);
-        mbar_init(&ds_ready, 8);
-        for (int i = 0; i < Cfg::kStages; ++i) { mbar_init(&full_bar[i], 1); mbar_init(&empty_bar[i], 1); }
+        for (uint64_t* bar : {&q_full, &do_full, &s_full[0], &s_full[1], &dp_full[0], &dp_full[1], &acc_full, &ragged_bar}) mbar_init(bar, 1);
+        for (uint64_t* bar : {&dp_read[0], &dp_read[1], &ds_ready[0], &ds_ready[1]}) mbar_init(bar, 4);
+        for (int i = 0; i < Cfg::kKeys; ++i) { mbar_init(&k_full[i], 1); mbar_init(&k_empty[i], 1); }
+        for (int i = 0; i < Cfg::kValues; ++i) { mbar_init(&v_full[i], 1); mbar_init(&v_empty[i], 1); }
         *abort_flag = 0;
         fence_mbar_init();
     }
@@ -791,129 +947,97 @@ attention_bwd_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
         registers_down<kAttnRegsDown>();
         if (warp == 9) {
             if (items && elect_one()) {
-                PipeState ps;
-                bool ok = true;
+                PipeState ks, vs;
                 attn_load<HD>(sQ, &tmQ, &q_full, head, first + q0);
-                for (int it = 0; it < items && ok; ++it) {
-#pragma unroll
-                    for (int g = 0; g < 2; ++g) {
-                        if (!mbar_wait(&empty_bar[ps.stage], ps.phase ^ 1u, abort_flag)) { ok = false; break; }
-                        attn_load<HD>(ring + ps.stage * Cfg::kTile, g ? &tmV : &tmK, ragged && g == 0 && it + 1 == items ? &ragged_bar : &full_bar[ps.stage], kv_head, first + (lo + it) * kAttnRows);
-                        ps.advance(Cfg::kStages);
-                        if (it == 0 && g == 0) attn_load<HD>(sdO, &tmdO, &do_full, head, first + q0);
-                    }
+                for (int it = 0; it < items; ++it) {
+                    const int row = first + (lo + it) * kAttnRows;
+                    if (!attn_wait(&k_empty[ks.stage], ks.phase ^ 1u, abort_flag)) break;
+                    attn_load<HD>(keys + ks.stage * Cfg::kTile, &tmK, ragged && it + 1 == items ? &ragged_bar : &k_full[ks.stage], kv_head, row);
+                    ks.advance(Cfg::kKeys);
+                    if (it == 0) attn_load<HD>(sdO, &tmdO, &do_full, head, first + q0);
+                    if (!attn_wait(&v_empty[vs.stage], vs.phase ^ 1u, abort_flag)) break;
+                    attn_load<HD>(values + vs.stage * Cfg::kTile, &tmV, &v_full[vs.stage], kv_head, row);
+                    vs.advance(Cfg::kValues);
                 }
             }
         } else if (warp == 8) {
             if (items && elect_one()) {
                 const int steps = (p.s.head_dim + 15) / 16;
-                const uint32_t idesc = make_idesc_bf16(kAttnRows, 16 * steps, false, true, false);
-                PipeState ps;
-                int k_stage = 0, k_next = 0, v_stage = 0;
-                const auto ready = [&](int& stage) {
-                    stage = ps.stage;
-                    const bool got = mbar_wait(&full_bar[ps.stage], ps.phase, abort_flag);
-                    ps.advance(Cfg::kStages);
-                    return got;
+                const uint32_t idesc = attn_row_idesc(p.s.head_dim);
+                const uint64_t q_desc = attn_column_desc(sQ), do_desc = attn_column_desc(sdO), key_desc = attn_column_desc(keys),
+                               key_rows = attn_row_desc(keys), value_desc = attn_column_desc(values);
+                PipeState ks, vs;                         // of the next scores and of the next products
+                const auto scores = [&](int it) {
+                    if (!attn_wait(&k_full[ks.stage], ks.phase, abort_flag)) return false;
+                    tc_fence_after_sync();
+                    attn_mma_columns<HD>(tmem + (it & 1) * kAttnRows, q_desc, key_desc + ks.stage * (Cfg::kTile >> 4), steps);
+                    umma_commit(&s_full[it & 1]);
+                    ks.advance(Cfg::kKeys);
+                    return true;
                 };
-                const auto at = [&](int stage) { return smem_u32(ring + stage * Cfg::kTile); };
-                bool ok = mbar_wait(&q_full, 0, abort_flag) && ready(k_stage);
-                if (ok) {
+                const auto products = [&](int it) {
+                    if (!attn_wait(&v_full[vs.stage], vs.phase, abort_flag)) return false;
                     tc_fence_after_sync();
-                    attn_mma_columns<HD>(tmem, smem_u32(sQ), at(k_stage), steps);
-                    umma_commit(&s_full[0]);
-                    ok = mbar_wait(&do_full, 0, abort_flag) && ready(v_stage);
-                }
-                if (ok) {
-                    tc_fence_after_sync();
-                    attn_mma_columns<HD>(t_dp, smem_u32(sdO), at(v_stage), steps);
-                    umma_commit(&dp_full);
-                    umma_commit(&empty_bar[v_stage]);
-                }
+                    attn_mma_columns<HD>(t_dp, do_desc, value_desc + vs.stage * (Cfg::kTile >> 4), steps);
+                    umma_commit(&dp_full[it & 1]);
+                    umma_commit(&v_empty[vs.stage]);
+                    vs.advance(Cfg::kValues);
+                    return true;
+                };
+                bool ok = attn_wait(&q_full, 0, abort_flag) && scores(0) && attn_wait(&do_full, 0, abort_flag) && products(0) && (items < 2 || scores(1));
                 for (int it = 0; it < items && ok; ++it) {
-                    const uint32_t t_s = tmem + (it & 1) * kAttnRows;
-                    const int rows = ragged && it + 1 == items ? last_rows : kAttnRows;
-                    if (it + 1 < items) {
-                        if (!(ok = ready(k_next))) break;
-                        tc_fence_after_sync();
-                        attn_mma_columns<HD>(tmem + ((it + 1) & 1) * kAttnRows, smem_u32(sQ), at(k_next), steps);
-                        umma_commit(&s_full[(it + 1) & 1]);
-                    }
-                    if (!(ok = mbar_wait(&ds_ready, it & 1, abort_flag))) break;
+                    const int rows = ragged && it + 1 == items ? last_rows : kAttnRows, g = it & 1, stage = it % Cfg::kKeys;
+                    const uint32_t t_s = tmem + g * kAttnRows, phase = (it >> 1) & 1;
+                    if (!(ok = attn_wait(&dp_read[g], phase, abort_flag) && (it + 1 >= items || products(it + 1)) && attn_wait(&ds_ready[g], phase, abort_flag)))
+                        break;
                     tc_fence_after_sync();
-                    attn_mma_rows(t_dq, t_s, t_s + 64, at(k_stage), idesc, (rows + 15) / 16, it != 0);
-                    umma_commit(it + 1 < items ? &empty_bar[k_stage] : &acc_full);
-                    if (it + 1 < items) {
-                        if (!(ok = ready(v_stage))) break;
-                        tc_fence_after_sync();
-                        attn_mma_columns<HD>(t_dp, smem_u32(sdO), at(v_stage), steps);
-                        umma_commit(&dp_full);
-                        umma_commit(&empty_bar[v_stage]);
-                    }
-                    k_stage = k_next;
+                    attn_mma_rows(t_dq, t_s, t_s + 64, key_rows + stage * (Cfg::kTile >> 4), idesc, (rows + 15) / 16, it != 0);
+                    umma_commit(it + 1 < items ? &k_empty[stage] : &acc_full);
+                    if (it + 2 < items) ok = scores(it + 2);
                 }
             }
         } else if (warp == 10 && ragged) {
-            const int stage = 2 * (items - 1) % Cfg::kStages;
+            const int stage = (items - 1) % Cfg::kKeys;
             if (warp_wait(&ragged_bar, 0, abort_flag)) {
-                attn_zero_rows<HD>(ring + stage * Cfg::kTile, last_rows);
-                warp_arrive(&full_bar[stage]);
+                attn_zero_rows<HD>(keys + stage * Cfg::kTile, last_rows);
+                warp_arrive(&k_full[stage]);
             }
         }
     } else {
         registers_up<kAttnRegsUp>();
         const int row = threadIdx.x & 127, i = q0 + row;
-        const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16, half = 64 * group;
+        const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
         float lse = 0.0f, delta = 0.0f;
         if (items && i < len) {
             const size_t at = static_cast<size_t>(head) * p.s.b + first + i;
             lse = __uint_as_float(ld_u32(p.lse + at)) * kLog2e;
             delta = __uint_as_float(ld_u32(p.delta + at));
         }
-        const Pair by = both(p.s.scale), less = both(-lse), minus = both(-delta);
         bool ok = items > 0;
-        for (int it = 0; it < items; ++it) {
+        for (int it = group; it < items; it += 2) {
             const int c0 = (lo + it) * kAttnRows;
             const bool edge = (p.s.causal ? c0 + kAttnRows - 1 > q0 : c0 + kAttnRows > len) || (p.s.window && q0 + kAttnRows - 1 - c0 >= p.s.window);
-            const int c_hi = (p.s.causal ? min(i + 1, len) : len) - c0 - static_cast<int>(half);
-            const int c_lo = p.s.window ? i - p.s.window + 1 - c0 - static_cast<int>(half) : 0;
-            const uint32_t s_row = tmem + (it & 1) * kAttnRows + lanes + half, dp_row = t_dp + lanes + half;
-            if (!(ok = warp_wait(&s_full[it & 1], (it >> 1) & 1, abort_flag))) break;
+            const int c_hi = (p.s.causal ? min(i + 1, len) : len) - c0, c_lo = p.s.window ? i - p.s.window + 1 - c0 : 0;
+            const uint32_t s_row = tmem + group * kAttnRows + lanes, dp_row = t_dp + lanes, phase = (it >> 1) & 1;
+            if (!(ok = warp_wait(&s_full[group], phase, abort_flag))) break;
             tc_fence_after_sync();
-            uint32_t v[64], g[64];
-            tmem_ld_32(s_row, v);
-            tmem_ld_32(s_row + 32, v + 32);
-            tmem_ld_wait();
-#pragma unroll
-            for (int c = 0; c < 64; c += 2) {
-                const Pair x = fma2(pair(v[c], v[c + 1]), by, less);
-                v[c] = __float_as_uint(exp2_fast(low(x)));
-                v[c + 1] = __float_as_uint(exp2_fast(high(x)));
-            }
-            if (!(ok = warp_wait(&dp_full, it & 1, abort_flag))) break;
+            uint32_t v[kAttnRows];
+            if (edge) attn_row_powers<true>(s_row, v, p.s.scale, lse, c_lo, c_hi);
+            else attn_row_powers<false>(s_row, v, p.s.scale, lse, 0, kAttnRows);
+            if (!(ok = warp_wait(&dp_full[group], phase, abort_flag))) break;
             tc_fence_after_sync();
-            tmem_ld_32(dp_row, g);
-            tmem_ld_32(dp_row + 32, g + 32);
-            tmem_ld_wait();
-#pragma unroll
-            for (int c = 0; c < 64; c += 2) {
-                const Pair y = mul2(pair(v[c], v[c + 1]), add2(pair(g[c], g[c + 1]), minus));
-                v[c >> 1] = pack_bf16x2(low(y), high(y));
-            }
-            if (edge) {
-#pragma unroll
-                for (int c = 0; c < 64; ++c)
-                    if (c < c_lo || c >= c_hi) v[c >> 1] &= c & 1 ? 0x0000FFFFu : 0xFFFF0000u;
-            }
+            if (edge) attn_row_gradients<true>(dp_row, v, delta, &dp_read[group], c_lo, c_hi);
+            else attn_row_gradients<false>(dp_row, v, delta, &dp_read[group], 0, kAttnRows);
             tmem_st_32(s_row, v);
+            tmem_st_32(s_row + 64, v + 32);
             tmem_st_wait();
             tc_fence_before_sync();
-            warp_arrive(&ds_ready);
+            warp_arrive(&ds_ready[group]);
         }
         if (ok && warp_wait(&acc_full, 0, abort_flag)) {
             tc_fence_after_sync();
             const size_t at = static_cast<size_t>(first) + q0;
-            attn_store<HD>(t_dq + lanes, group * HD / 2, (group + 1) * HD / 2, p.grad_scale, group ? sdO : sQ,
+            attn_store<HD, HD / 2>(t_dq + lanes, group * HD / 2, p.grad_scale, group ? sdO : sQ,
                            p.dQ + at * p.dq_ld + head * p.s.head_dim, p.dq_ld, len - q0, p.s.head_dim);
         }
         tc_fence_before_sync();
