@@ -35,9 +35,10 @@ static slope_status_t attn_batch(AttnShape* s, int b, int heads, int kv_heads, i
                                  int causal, int window, float scale) {
     if (!(scale > 0.0f && scale <= FLT_MAX) || window < 0 || (window && !causal)) return SLOPE_ERR_INVALID_ARG;
     if (!heads_ok(b, heads, kv_heads, head_dim) || sequences < 1 || (!starts && b % sequences != 0)) return SLOPE_ERR_SHAPE;
-    if (attn_units(b, sequences, starts, kAttnRows) * heads > INT_MAX) return SLOPE_ERR_SHAPE;
+    if (attn_units(b, sequences, starts, kAttnRows) * (heads + kv_heads) > INT_MAX) return SLOPE_ERR_SHAPE;
     *s = AttnShape{b, heads, kv_heads, head_dim, sequences, static_cast<const int*>(starts), static_cast<const int*>(lengths), causal != 0,
-                   window < b ? window : 0, scale * kLog2e};
+                   window < b ? window : 0, scale * kLog2e, heads / kv_heads, b / sequences, 1.0f / heads, 1.0f / kv_heads,
+                   static_cast<float>(kv_heads) / heads};
     return SLOPE_OK;
 }
 template <typename Kernel, typename... Args>
@@ -51,23 +52,22 @@ static slope_status_t attn_fwd(const AttnFwdParams& p, const CUtensorMap (&tm)[3
                        AttnCfg<HD>::kSmem, stream, tm[0], tm[1], tm[2], p);
 }
 template <int HD>
-static slope_status_t attn_bwd(const AttnBwdParams& p, const AttnDeltaParams& d, const CUtensorMap (&tm)[4], cudaStream_t stream) {
+static slope_status_t attn_bwd(AttnBwdParams p, const AttnDeltaParams& d, const CUtensorMap (&tm)[4], cudaStream_t stream) {
+    const long long units = attn_units(p.s.b, p.s.sequences, p.s.starts, kAttnRows);
+    p.key_blocks = static_cast<int>(units * p.s.kv_heads);
     const long long blocks = static_cast<long long>((p.s.b - 1) / 32 + 1) * ((p.s.heads + 7) / 8);
     if (slope_status_t st = launch_cluster_ex(attention_delta_kernel<HD>, static_cast<int>(blocks), 1, 256, 0, /*overlap_prologue=*/true, stream, d)) return st;
-    const long long units = attn_units(p.s.b, p.s.sequences, p.s.starts, kAttnRows);
-    // tiles begin on a multiple of 1 KB behind what has a fixed place
-    constexpr int kKvFixed = sizeof(AttnKvShared<AttnCfg<HD>::kStages>), kKvSmem = (2 + AttnCfg<HD>::kStages) * AttnCfg<HD>::kTile + (kKvFixed + 1023) / 1024 * 1024 - kKvFixed;
-    static_assert(kKvFixed % 16 == 0 && kKvFixed + kKvSmem <= 227 * 1024, "shared memory of the kernel of dK and dV");
-    if (slope_status_t st = launch_attn(attention_bwd_kv_kernel<HD>, units * p.s.kv_heads, kAttnThreads, kKvSmem, stream, tm[0], tm[1], tm[2], tm[3], p))
-        return st;
-    return launch_attn(attention_bwd_q_kernel<HD>, units * p.s.heads, kAttnThreads, AttnCfg<HD>::kSmem, stream, tm[0], tm[1], tm[2], tm[3], p);
+    // tiles begin on a multiple of 1 KB behind what has a fixed place (which ends on a multiple of 128 bytes, as dynamic shared memory begins)
+    constexpr int kFixed = sizeof(AttnBwdShared<HD>), kSmem = (2 + AttnCfg<HD>::kStages) * AttnCfg<HD>::kTile + (kFixed + 1023) / 1024 * 1024 - kFixed;
+    static_assert(kFixed % 128 == 0 && kFixed + kSmem <= 227 * 1024, "shared memory of a block");
+    return launch_attn(attention_bwd_kernel<HD>, p.key_blocks + units * p.s.heads, kAttnThreads, kSmem, stream, tm[0], tm[1], tm[2], tm[3], p);
 }
 template <int TYPE, bool PAIRS>
 static slope_status_t launch_rotary(const RotaryParams& p, int wide, cudaStream_t stream) {
-    const auto kern = wide == 8   ? rotary_kernel<TYPE, PAIRS, 8>
-                      : wide == 4 ? rotary_kernel<TYPE, PAIRS, 4>
-                      : wide == 2 ? rotary_kernel<TYPE, PAIRS, 2>
-                                  : rotary_kernel<TYPE, PAIRS, PAIRS ? 2 : 1>;
+    const auto kern = PAIRS || wide == 8 ? rotary_kernel<TYPE, PAIRS, 8>
+                      : wide == 4        ? rotary_kernel<TYPE, false, 4>
+                      : wide == 2        ? rotary_kernel<TYPE, false, 2>
+                                         : rotary_kernel<TYPE, false, 1>;
     return launch_cluster_ex(kern, (p.b - 1) / p.tokens + 1, 1, kRotaryThreads, 0, /*overlap_prologue=*/true, stream, p);
 }
 }  // namespace slope
@@ -122,7 +122,7 @@ slope_status_t slope_attention_bwd(const void* dO, int do_ld, const void* Q, int
         return SLOPE_ERR_CUDA;
     float* delta = static_cast<float*>(workspace);
     const AttnBwdParams p{s,    static_cast<const float*>(lse), delta, static_cast<uint16_t*>(dQ), static_cast<uint16_t*>(dK), static_cast<uint16_t*>(dV),
-                          dq_ld, dk_ld, dv_ld, scale};
+                          dq_ld, dk_ld, dv_ld, scale, 0};
     const AttnDeltaParams d{static_cast<const uint16_t*>(O), static_cast<const uint16_t*>(dO), o_ld, do_ld, b, heads, head_dim, delta};
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     return head_dim <= 64 ? attn_bwd<64>(p, d, tm, stream) : attn_bwd<128>(p, d, tm, stream);
@@ -149,7 +149,7 @@ slope_status_t slope_rotary(const void* Q, int q_ld, const void* K, int k_ld, in
     const long long most = std::min<long long>({kRotaryThreads / p.n, b / (4ll * info.sm_count), 8 * kRotaryThreads / tasks, 64});
     p.tokens = static_cast<int>(std::max(1ll, most));
     // as many values at a time as the rotated part is a multiple of
-    const int unit = interleaved ? rot_dim : rot_dim / 2, wide = unit % 8 == 0 ? 8 : unit % 4 == 0 ? 4 : unit % 2 == 0 ? 2 : 1;
+    const int wide = interleaved || p.n % 8 == 0 ? 8 : p.n % 4 == 0 ? 4 : p.n % 2 == 0 ? 2 : 1;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (type == SLOPE_F32) return interleaved ? launch_rotary<kTypeF32, true>(p, wide, s) : launch_rotary<kTypeF32, false>(p, wide, s);
     return interleaved ? launch_rotary<kTypeBf16, true>(p, wide, s) : launch_rotary<kTypeBf16, false>(p, wide, s);

@@ -90,6 +90,8 @@ struct AttnShape {
     const int *starts, *lengths;
     int causal, window;
     float scale;                          // of the products, times log2(e): probabilities are powers of two here
+    int share, part;                      // query heads of a key head; rows of a sequence, where all are equal
+    float per_heads, per_kv_heads, per_share;      // reciprocals
 };
 struct AttnTile {
     int first, len, tile;                 // the sequence's first row, its length, number of the tile of `rows` rows; len 0: nothing to do
@@ -101,16 +103,31 @@ constexpr int kAttnThreads = 384;         // two groups of four warps that compu
 constexpr int kAttnRegsUp = 208, kAttnRegsDown = 88;
 static_assert(2 * kAttnRegsUp + kAttnRegsDown == 3 * 168, "shares of the launch's registers");
 
+// x / d and what is left, x >= 0, with the reciprocal at hand (a division takes 100 clocks, and a block has four in front of its first load).
+struct AttnQuotient {
+    int quotient, rest;
+};
+__device__ __forceinline__ AttnQuotient attn_divide(int x, int d, float per_d) {
+    AttnQuotient r;
+    r.quotient = static_cast<int>(static_cast<float>(x) * per_d);
+    r.rest = x - r.quotient * d;                                     // (2^-23 of the quotient off, at most, and one)
+    while (r.rest < 0) { --r.quotient; r.rest += d; }
+    while (r.rest >= d) { ++r.quotient; r.rest -= d; }
+    return r;
+}
 // Tile number `unit` of the call, the last tile of a sequence first where later rows see more keys.  By one whole warp.
-__device__ __forceinline__ AttnTile attn_locate(const AttnShape& s, int unit, int rows, bool last_first) {
+template <int ROWS>
+__device__ __forceinline__ AttnTile attn_locate(const AttnShape& s, int unit, bool last_first) {
+    constexpr int rows = ROWS;
     const int lane = threadIdx.x & 31;
     AttnTile t{0, 0, 0};
     int n = 0, rank = 0;
     if (!s.starts) {
-        const int part = s.b / s.sequences, tiles = (part - 1) / rows + 1, seq = unit / tiles;
-        rank = unit - seq * tiles;
-        t.first = seq * part;
-        t.len = s.lengths ? min(max(s.lengths[seq], 0), part) : part;
+        const int tiles = (s.part - 1) / rows + 1;
+        const AttnQuotient q = attn_divide(unit, tiles, 1.0f / static_cast<float>(tiles));
+        rank = q.rest;
+        t.first = q.quotient * s.part;
+        t.len = s.lengths ? min(max(s.lengths[q.quotient], 0), s.part) : s.part;
         n = (t.len + rows - 1) / rows;
         if (rank >= n) t.len = 0;
     } else {
@@ -166,19 +183,32 @@ struct AttnCfg {
     static constexpr int kChunks = HD / 64, kTile = kChunks * kAttnChunk;
     static constexpr int kStages = HD == 128 ? 5 : 8;           // of the ring, beside two tiles that stay
     static constexpr int kSmem = (2 + kStages) * kTile + 1024;
-    // of the kernel of dQ: places for K, which stay until dQ has them, and for V
+    // of a block of dQ: places for K, which stay until dQ has them, and for V
     static constexpr int kKeys = HD == 128 ? 3 : 4, kValues = kStages - kKeys;
 };
-// What the kernel of dK and dV has beside its tiles.
+// What a block of dK and dV has beside its tiles ...
 template <int STAGES>
-struct alignas(16) AttnKvShared {
+struct alignas(128) AttnKvShared {
     uint4 minus_d[kAttnRows];             // of a tile's queries: -D / 2 as a sum of three bf16 values, zeros behind them
     uint4 ones[8];                        // eight rows of three ones
     float lse[kAttnRows];                 // in powers of two
-    uint64_t k_full, v_full, acc_full, s_full[2], s_read[2], dp_full[2], pairs_full[2], powers_done, d_full, full[STAGES], empty[STAGES], ragged[STAGES];
+    uint64_t k_full, v_full, acc_full, s_full[2], s_read[2], dp_full[2], pairs_full[2][2], powers_done, d_full, full[STAGES], empty[STAGES], ragged[STAGES];
     uint32_t tmem;
     int abort_word;
     AttnTile work;
+};
+// ... and that of dQ
+template <int KEYS, int VALUES>
+struct alignas(128) AttnQShared {
+    uint64_t q_full, do_full, s_full[2], dp_full[2], dp_read[2], ds_ready[2], acc_full, ragged_bar, k_full[KEYS], k_empty[KEYS], v_full[VALUES], v_empty[VALUES];
+    uint32_t tmem;
+    int abort_word;
+    AttnTile work;
+};
+template <int HD>
+union AttnBwdShared {
+    AttnKvShared<AttnCfg<HD>::kStages> keys;
+    AttnQShared<AttnCfg<HD>::kKeys, AttnCfg<HD>::kValues> queries;
 };
 template <int HD>
 __device__ __forceinline__ void attn_load(uint8_t* tile, const CUtensorMap* tm, uint64_t* bar, int head, int row) {
@@ -226,6 +256,11 @@ __device__ __forceinline__ void attn_mma_rows(uint32_t d, uint32_t a0, uint32_t 
 }
 // of a product whose B is [rows x head]
 __device__ __forceinline__ uint32_t attn_row_idesc(int head_dim) { return make_idesc_bf16(kAttnRows, (head_dim + 15) & ~15, false, true, false); }
+// Bits [lo, hi) of 32: which of 32 columns are seen.  (A bit of a register as a condition is half of what two comparisons cost.)
+__device__ __forceinline__ uint32_t attn_bits(int lo, int hi) {
+    const uint32_t below_hi = hi >= 32 ? 0xFFFFFFFFu : hi <= 0 ? 0u : (1u << hi) - 1u, below_lo = lo >= 32 ? 0xFFFFFFFFu : lo <= 0 ? 0u : (1u << lo) - 1u;
+    return below_hi & ~below_lo;
+}
 // Rows [valid, 16-multiple) of a tile to zero: they belong to other sequences or to none, and what stands there may be an infinity or a NaN,
 // which a probability of zero does not take out of a product.  Such a tile's copies complete on a barrier of its own, for one warp that zeroes the
 // rows and then completes the barrier that the tile's readers wait for.
@@ -303,9 +338,10 @@ __device__ __forceinline__ float attn_scores(uint32_t s_row, uint32_t (&v)[kAttn
         if (c == 0) tmem_ld_wait_32(v);
         else tie_32(v + c);
         if (EDGE) {
+            const uint32_t bits = attn_bits(lo - c, hi - c);
 #pragma unroll
-            for (int k = c; k < c + 32; ++k)
-                if (k < lo || k >= hi) v[k] = 0xFF800000u;
+            for (int k = 0; k < 32; ++k)
+                if (!(bits >> k & 1u)) v[c + k] = 0xFF800000u;
         }
 #pragma unroll
         for (int k = c; k < c + 32; k += 2) top[(k >> 1) & 3] = max3(top[(k >> 1) & 3], __uint_as_float(v[k]), __uint_as_float(v[k + 1]));
@@ -334,7 +370,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
 attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                      const AttnFwdParams p) {
     using Cfg = AttnCfg<HD>;
-    __shared__ uint64_t q_full[2], s_full[2], p_full[2][2], o_full[2], full_bar[Cfg::kStages], empty_bar[Cfg::kStages], ragged_bar;
+    __shared__ uint64_t q_full[2], s_full[2], s_read[2], p_full[2][2], pv_done[2], o_full[2], full_bar[Cfg::kStages], empty_bar[Cfg::kStages], ragged_bar;
     __shared__ uint32_t tmem_slot[1];
     __shared__ int abort_word;
     __shared__ AttnTile work;
@@ -349,6 +385,8 @@ attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         for (int t = 0; t < 2; ++t) {
             mbar_init(&q_full[t], 1);
             mbar_init(&s_full[t], 1);
+            mbar_init(&s_read[t], 4);
+            mbar_init(&pv_done[t], 1);
             mbar_init(&p_full[t][0], 4);
             mbar_init(&p_full[t][1], 4);
             mbar_init(&o_full[t], 1);
@@ -362,16 +400,24 @@ attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         tmem_alloc(tmem_slot, 512);
         tmem_relinquish();
     }
-    griddep_wait();
-    const int head = blockIdx.x % p.s.heads, kv_head = head / (p.s.heads / p.s.kv_heads);
+    const AttnQuotient unit = attn_divide(blockIdx.x, p.s.heads, p.s.per_heads);
+    const int head = unit.rest, kv_head = attn_divide(head, p.s.share, p.s.per_share).quotient;
+    // (sequences that the host knows are found beside the preceding kernel's end)
+    const bool known = !p.s.starts && !p.s.lengths;
+    if (!known) griddep_wait();
     if (warp == 0) {
-        const AttnTile t = attn_locate(p.s, blockIdx.x / p.s.heads, 2 * kAttnRows, p.s.causal);
+        const AttnTile t = attn_locate<2 * kAttnRows>(p.s, unit.quotient, p.s.causal);
         if (lane == 0) work = t;
     }
+    if (known) griddep_wait();
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
-    const uint32_t tmem = *tmem_slot;                      // S of either tile, then O of either; P lies over the first and third quarter of S
+    // S of either tile, then O of either.  P: over the first and third quarter of S; where a head has 64 columns, behind O, so that the next scores wait
+    // for these ones to be read only (us, 4 x 4096 tokens, 16 heads: over / apart 384 / 340)
+    constexpr bool kApart = HD == 64;
+    const uint32_t tmem = *tmem_slot;
+    const auto p_at = [&](int t, int h) { return kApart ? tmem + 3 * kAttnRows + 64 * t + 32 * h : tmem + kAttnRows * t + 64 * h; };
     const int len = work.len, first = work.first, q0 = work.tile * 2 * kAttnRows;
     const int tiles = !len ? 0 : len - q0 > kAttnRows ? 2 : 1;
     // tiles of keys [lo, hi) of the two tiles of queries and of both
@@ -436,19 +482,26 @@ attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                     }
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
+                        const bool next = lo[t] <= j + 1 && j + 1 < hi[t];
+                        if (kApart && next) {
+                            if (lo[t] <= j && !(ok = ok && attn_wait(&s_read[t], phase[t], abort_flag))) continue;
+                            tc_fence_after_sync();
+                            scores(t, k_stage);
+                        }
                         if (lo[t] <= j && j < hi[t]) {
-                            const uint32_t s = tmem + t * kAttnRows, o = tmem + 2 * kAttnRows + t * HD;
+                            const uint32_t o = tmem + 2 * kAttnRows + t * HD;
                             const uint64_t v = row_desc + v_stage * (Cfg::kTile >> 4);
                             if (!(ok = ok && attn_wait(&p_full[t][0], phase[t], abort_flag))) continue;
                             tc_fence_after_sync();
-                            attn_mma_rows(o, s, v, idesc, (rows + 15) / 16, j != lo[t]);
+                            attn_mma_rows(o, p_at(t, 0), v, idesc, (rows + 15) / 16, j != lo[t]);
                             if (!(ok = attn_wait(&p_full[t][1], phase[t], abort_flag))) continue;
                             tc_fence_after_sync();
-                            attn_mma_rows(o, s + 64, v + (64 * 128 >> 4), idesc, (rows + 15) / 16 - 4, true);
+                            attn_mma_rows(o, p_at(t, 1), v + (64 * 128 >> 4), idesc, (rows + 15) / 16 - 4, true);
+                            if (kApart) umma_commit(&pv_done[t]);
                             phase[t] ^= 1u;
                             if (j + 1 == hi[t]) umma_commit(&o_full[t]);
                         }
-                        if (lo[t] <= j + 1 && j + 1 < hi[t]) scores(t, k_stage);
+                        if (!kApart && next) scores(t, k_stage);
                     }
                     if (!ok) break;
                     umma_commit(&empty_bar[v_stage]);
@@ -483,11 +536,17 @@ attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                 now = attn_scores<true>(s_row, v, p.s.window ? i - p.s.window + 1 - c0 : 0, (p.s.causal ? min(i + 1, len) : len) - c0) * by;
             else
                 now = attn_scores<false>(s_row, v, 0, kAttnRows) * by;
+            if (kApart) {
+                tc_fence_before_sync();
+                warp_arrive(&s_read[t]);
+                // the last P V: P is free, O may be rescaled.  (Otherwise it has completed with these scores.)
+                if (j != j_lo && !(ok = warp_wait(&pv_done[t], phase, abort_flag))) break;
+                tc_fence_after_sync();
+            }
             if (__any_sync(0xFFFFFFFFu, now > m + kAttnSlack)) {
                 const float next = fmaxf(m, now), part = next == m ? 1.0f : exp2_fast(m - next);
                 m = next;
                 l *= part;
-                // (the last P V has completed with these scores)
 #pragma unroll 1
                 for (int c = 0; c < (j == j_lo ? 0 : p.s.head_dim); c += 32) {
                     uint32_t o[32];
@@ -504,7 +563,7 @@ attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             for (int h = 0; h < 2; ++h) {
                 uint32_t w[32];
                 attn_probabilities(v + 64 * h, w, by, less, sum);
-                tmem_st_32(s_row + 64 * h, w);
+                tmem_st_32(p_at(t, h) + lanes, w);
                 tmem_st_wait();
                 tc_fence_before_sync();
                 warp_arrive(&p_full[t][h]);
@@ -532,7 +591,8 @@ attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
 // =====================================================================================
 // Backward.  With D = rowsum(dO O), P = 2^(scale S - lse) and dS = P (dO V^T - D):
 //   dV = P^T dO,   dK = scale dS^T Q (sums over queries and over the heads that share a key head),   dQ = scale dS K (a sum over keys).
-// Two kernels form S and dP = dO V^T once each: with a third more products nothing is added up in memory, so that every sum has a fixed order.
+// Blocks of keys and blocks of queries form S and dP = dO V^T once each: with two fifths more products nothing is added up in memory, and every sum has
+// a fixed order.
 // =====================================================================================
 // D of every row and head, [heads x b].  A group of HD / 8 lanes takes a head of a row; 32 rows of a block go out together.
 struct AttnDeltaParams {
@@ -576,6 +636,7 @@ struct AttnBwdParams {
     uint16_t *dQ, *dK, *dV;
     int dq_ld, dk_ld, dv_ld;
     float grad_scale;                     // the products' factor itself
+    int key_blocks;                       // blocks of dK and dV
 };
 
 // A key's 128 scores -> 2^(v by - lse): lse belongs to the query, the column, and lies in shared memory ...  EDGE: those outside [lo, hi) are 0 (two
@@ -593,8 +654,12 @@ __device__ __forceinline__ void attn_column_powers(uint32_t (&v)[kAttnRows], flo
     }
     if (EDGE) {
 #pragma unroll
-        for (int c = 0; c < kAttnRows; ++c)
-            if (c < lo || c >= hi) v[c] = 0u;
+        for (int c = 0; c < kAttnRows; c += 32) {
+            const uint32_t bits = attn_bits(lo - c, hi - c);
+#pragma unroll
+            for (int k = 0; k < 32; ++k)
+                if (!(bits >> k & 1u)) v[c + k] = 0u;
+        }
     }
 }
 // ... and, with dP - D from tensor memory, to bf16 pairs: 32 values of P and behind them 32 of dS = P (dP - D) at a time, in the place of dP; the
@@ -613,9 +678,10 @@ __device__ __forceinline__ void attn_column_pairs(uint32_t dp_row, uint32_t (&v)
             g[k >> 1] = pack_bf16x2(low(y), high(y));
         }
         if (EDGE) {                                         // (zero times what a row of no sequence holds)
+            const uint32_t bits = attn_bits(lo - c, hi - c);
 #pragma unroll
             for (int k = 0; k < 32; ++k)
-                if (c + k < lo || c + k >= hi) g[k >> 1] &= k & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+                if (!(bits >> k & 1u)) g[k >> 1] &= k & 1 ? 0x0000FFFFu : 0xFFFF0000u;
         }
         tmem_st_16(dp_row + c, v + c);
         tmem_st_16(dp_row + c + 16, g);
@@ -642,15 +708,10 @@ __device__ __forceinline__ uint4 attn_split(float x) {
 // What bounds it is the way dP - dS - dV, dK - next dP, 2000 of whose clocks at 128 columns are the products' (2048 with S).
 // Warp 11: the MMAs of S; 8: the others; 9: loads; 10: lse and D, zeros behind the sequence's last row.
 template <int HD>
-__global__ void __launch_bounds__(kAttnThreads, 1)
-attention_bwd_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-                        const __grid_constant__ CUtensorMap tmdO, const AttnBwdParams p) {
+__device__ __forceinline__ void attn_bwd_keys(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmdO,
+                                              const AttnBwdParams& p, int block, AttnKvShared<AttnCfg<HD>::kStages>& sh, uint8_t* smem) {
     using Cfg = AttnCfg<HD>;
-    // (one array, whose size the host knows: beside seven tiles of 128 columns there are 3 KB)
-    __shared__ AttnKvShared<Cfg::kStages> sh;
     volatile int* abort_flag = &sh.abort_word;
-    extern __shared__ uint8_t smem_raw[];
-    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t *sK = smem, *sV = smem + Cfg::kTile, *ring = smem + 2 * Cfg::kTile;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = threadIdx.x >> 7;
 
@@ -660,7 +721,8 @@ attention_bwd_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sh.s_full[i], 2);                    // the scores, and what belongs to their queries
             mbar_init(&sh.s_read[i], 4);
-            mbar_init(&sh.pairs_full[i], 4);
+            mbar_init(&sh.pairs_full[i][0], 4);
+            mbar_init(&sh.pairs_full[i][1], 4);
         }
         mbar_init(&sh.powers_done, 4);
         for (int i = 0; i < Cfg::kStages; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); mbar_init(&sh.ragged[i], 1); }
@@ -675,16 +737,22 @@ attention_bwd_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
         tmem_alloc(&sh.tmem, 512);
         tmem_relinquish();
     }
-    griddep_wait();
-    const int kv_head = blockIdx.x % p.s.kv_heads, share = p.s.heads / p.s.kv_heads;
+    const AttnQuotient unit = attn_divide(block, p.s.kv_heads, p.s.per_kv_heads);
+    const int kv_head = unit.rest, share = p.s.share;
+    const bool known = !p.s.starts && !p.s.lengths;
+    if (!known) griddep_wait();
     if (warp == 0) {
-        const AttnTile t = attn_locate(p.s, blockIdx.x / p.s.kv_heads, kAttnRows, false);
+        const AttnTile t = attn_locate<kAttnRows>(p.s, unit.quotient, false);
         if (lane == 0) sh.work = t;
     }
+    if (known) griddep_wait();
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
-    const uint32_t tmem = sh.tmem, t_s = tmem, t_dp = tmem + kAttnRows, t_dv = tmem + 2 * kAttnRows, t_dk = t_dv + HD;
+    // S, dP, dV, dK; where a head has 64 columns another place for dP, which then waits for nothing of the item before
+    constexpr bool kTwo = HD == 64;
+    const uint32_t tmem = sh.tmem, t_s = tmem, t_dv = tmem + 2 * kAttnRows, t_dk = t_dv + HD;
+    const auto dp_at = [&](int it) { return tmem + (kTwo && (it & 1) ? 3 * kAttnRows : kAttnRows); };
     const int len = sh.work.len, first = sh.work.first, k0 = sh.work.tile * kAttnRows;
     // an item: a tile of queries of one of the heads that share the key head
     const int lo = attn_first_query_tile(p.s, k0), hi = len ? attn_end_query_tile(p.s, k0, len) : lo, items = (hi - lo) * share;
@@ -735,35 +803,39 @@ attention_bwd_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                 const uint64_t v_desc = attn_column_desc(sV), column_desc = attn_column_desc(ring), row_desc = attn_row_desc(ring);
                 // rows of eight values without a swizzle, the same eight for both eighths of the step; the same eight rows of ones throughout
                 const uint64_t ones_desc = make_smem_desc(smem_u32(sh.ones), 0, 0, kSwizzleNone), d_desc = make_smem_desc(smem_u32(sh.minus_d), 0, 128, kSwizzleNone);
-                PipeState qs, os;                         // places of this item's Q and dO
+                PipeState qs, os;                         // places of an item's Q, and of the next products' dO
                 os.advance(Cfg::kStages);
                 // (behind `d_full` dO is there, too)
                 const auto products = [&](int it) {
                     if (!attn_wait(&sh.d_full, it & 1, abort_flag)) return false;
                     tc_fence_after_sync();
-                    umma_bf16(t_dp, ones_desc, d_desc, make_idesc_bf16(kAttnRows, kAttnRows, false, false, false), 0);
-                    attn_mma_columns<HD>(t_dp, v_desc, column_desc + os.stage * (Cfg::kTile >> 4), steps, true);
+                    umma_bf16(dp_at(it), ones_desc, d_desc, make_idesc_bf16(kAttnRows, kAttnRows, false, false, false), 0);
+                    attn_mma_columns<HD>(dp_at(it), v_desc, column_desc + os.stage * (Cfg::kTile >> 4), steps, true);
                     umma_commit(&sh.dp_full[it & 1]);
+                    os.advance(Cfg::kStages);
+                    os.advance(Cfg::kStages);
                     return true;
                 };
                 bool ok = attn_wait(&sh.v_full, 0, abort_flag) && products(0);
                 for (int it = 0, tile = lo; it < items && ok; ++it) {
-                    const int row_steps = (rows_of(tile) + 15) / 16;
+                    const int row_steps = (rows_of(tile) + 15) / 16, o_stage = qs.stage + 1 < Cfg::kStages ? qs.stage + 1 : 0;
                     if (++tile == hi) tile = lo;
+                    if (kTwo && it + 1 < items && !(ok = products(it + 1))) break;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        if (!(ok = ok && attn_wait(&sh.pairs_full[h], it & 1, abort_flag))) continue;
+                        if (!(ok = ok && attn_wait(&sh.pairs_full[it & 1][h], (it >> 1) & 1, abort_flag))) continue;
                         tc_fence_after_sync();
-                        const uint32_t a = t_dp + 64 * h, b = h * (64 * 128 >> 4);
-                        attn_mma_rows<32>(t_dv, a, row_desc + os.stage * (Cfg::kTile >> 4) + b, idesc, row_steps - 4 * h, it != 0 || h);
+                        const uint32_t a = dp_at(it) + 64 * h, b = h * (64 * 128 >> 4);
+                        attn_mma_rows<32>(t_dv, a, row_desc + o_stage * (Cfg::kTile >> 4) + b, idesc, row_steps - 4 * h, it != 0 || h);
                         attn_mma_rows<32>(t_dk, a + 16, row_desc + qs.stage * (Cfg::kTile >> 4) + b, idesc, row_steps - 4 * h, it != 0 || h);
                     }
                     if (!ok) break;
                     umma_commit(&sh.empty[qs.stage]);
-                    umma_commit(&sh.empty[os.stage]);
-                    for (int g = 0; g < 2; ++g) { qs.advance(Cfg::kStages); os.advance(Cfg::kStages); }
-                    if (it + 1 < items) ok = products(it + 1);
-                    else umma_commit(&sh.acc_full);
+                    umma_commit(&sh.empty[o_stage]);
+                    qs.advance(Cfg::kStages);
+                    qs.advance(Cfg::kStages);
+                    if (it + 1 == items) umma_commit(&sh.acc_full);
+                    else if (!kTwo) ok = products(it + 1);
                 }
             }
         } else if (warp == 10) {
@@ -807,7 +879,7 @@ attention_bwd_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
         registers_up<kAttnRegsUp>();
         const int key = k0 + (threadIdx.x & 127);
         const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-        const uint32_t s_row = t_s + lanes, dp_row = t_dp + lanes;
+        const uint32_t s_row = t_s + lanes, dp_row = dp_at(group) + lanes;
         bool ok = items > 0;
         for (int it = group, tile = lo + group; it < items; it += 2, tile += 2) {
             while (tile >= hi) tile -= hi - lo;
@@ -832,8 +904,8 @@ attention_bwd_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
             warp_arrive(&sh.powers_done);
             if (!(ok = warp_wait(&sh.dp_full[group], phase, abort_flag))) break;
             tc_fence_after_sync();
-            if (edge) attn_column_pairs<true>(dp_row, v, sh.pairs_full, c_lo, c_hi);
-            else attn_column_pairs<false>(dp_row, v, sh.pairs_full, 0, kAttnRows);
+            if (edge) attn_column_pairs<true>(dp_row, v, sh.pairs_full[group], c_lo, c_hi);
+            else attn_column_pairs<false>(dp_row, v, sh.pairs_full[group], 0, kAttnRows);
         }
         if (ok && warp_wait(&sh.acc_full, 0, abort_flag)) {
             tc_fence_after_sync();
@@ -864,8 +936,13 @@ __device__ __forceinline__ void attn_row_powers(uint32_t s_row, uint32_t (&v)[kA
 #pragma unroll
         for (int k = c; k < c + 32; k += 2) {
             const Pair x = fma2(pair(v[k], v[k + 1]), both(by), both(-lse));
-            v[k] = !EDGE || (k >= lo && k < hi) ? __float_as_uint(exp2_fast(low(x))) : 0u;
-            v[k + 1] = !EDGE || (k + 1 >= lo && k + 1 < hi) ? __float_as_uint(exp2_fast(high(x))) : 0u;
+            v[k] = __float_as_uint(exp2_fast(low(x)));
+            v[k + 1] = __float_as_uint(exp2_fast(high(x)));
+        }
+        if (EDGE) {
+#pragma unroll
+            for (int k = c; k < c + 32; ++k)
+                if (k < lo || k >= hi) v[k] = 0u;
         }
     }
 }
@@ -900,45 +977,40 @@ __device__ __forceinline__ void attn_row_gradients(uint32_t dp_row, uint32_t (&v
 // its dS.  S has a place for either group and is formed two tiles ahead; dS takes the place of S; dP is read as soon as it is there, so that the
 // next one is formed beside dS.  (Both groups on every tile, 64 keys each: 2400 clocks a tile.)
 template <int HD>
-__global__ void __launch_bounds__(kAttnThreads, 1)
-attention_bwd_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-                       const __grid_constant__ CUtensorMap tmdO, const AttnBwdParams p) {
+__device__ __forceinline__ void attn_bwd_queries(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmdO,
+                                                 const AttnBwdParams& p, int block, AttnQShared<AttnCfg<HD>::kKeys, AttnCfg<HD>::kValues>& sh, uint8_t* smem) {
     using Cfg = AttnCfg<HD>;
-    __shared__ uint64_t q_full, do_full, s_full[2], dp_full[2], dp_read[2], ds_ready[2], acc_full, ragged_bar;
-    __shared__ uint64_t k_full[Cfg::kKeys], k_empty[Cfg::kKeys], v_full[Cfg::kValues], v_empty[Cfg::kValues];
-    __shared__ uint32_t tmem_slot[1];
-    __shared__ int abort_word;
-    __shared__ AttnTile work;
-    volatile int* abort_flag = &abort_word;
-    extern __shared__ uint8_t smem_raw[];
-    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    volatile int* abort_flag = &sh.abort_word;
     uint8_t *sQ = smem, *sdO = smem + Cfg::kTile, *keys = smem + 2 * Cfg::kTile, *values = keys + Cfg::kKeys * Cfg::kTile;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = threadIdx.x >> 7;
 
     griddep_launch_dependents();
     if (threadIdx.x == 0) {
-        for (uint64_t* bar : {&q_full, &do_full, &s_full[0], &s_full[1], &dp_full[0], &dp_full[1], &acc_full, &ragged_bar}) mbar_init(bar, 1);
-        for (uint64_t* bar : {&dp_read[0], &dp_read[1], &ds_ready[0], &ds_ready[1]}) mbar_init(bar, 4);
-        for (int i = 0; i < Cfg::kKeys; ++i) { mbar_init(&k_full[i], 1); mbar_init(&k_empty[i], 1); }
-        for (int i = 0; i < Cfg::kValues; ++i) { mbar_init(&v_full[i], 1); mbar_init(&v_empty[i], 1); }
+        for (uint64_t* bar : {&sh.q_full, &sh.do_full, &sh.s_full[0], &sh.s_full[1], &sh.dp_full[0], &sh.dp_full[1], &sh.acc_full, &sh.ragged_bar}) mbar_init(bar, 1);
+        for (uint64_t* bar : {&sh.dp_read[0], &sh.dp_read[1], &sh.ds_ready[0], &sh.ds_ready[1]}) mbar_init(bar, 4);
+        for (int i = 0; i < Cfg::kKeys; ++i) { mbar_init(&sh.k_full[i], 1); mbar_init(&sh.k_empty[i], 1); }
+        for (int i = 0; i < Cfg::kValues; ++i) { mbar_init(&sh.v_full[i], 1); mbar_init(&sh.v_empty[i], 1); }
         *abort_flag = 0;
         fence_mbar_init();
     }
     if (warp == 8) {
-        tmem_alloc(tmem_slot, 512);
+        tmem_alloc(&sh.tmem, 512);
         tmem_relinquish();
     }
-    griddep_wait();
-    const int head = blockIdx.x % p.s.heads, kv_head = head / (p.s.heads / p.s.kv_heads);
+    const AttnQuotient unit = attn_divide(block, p.s.heads, p.s.per_heads);
+    const int head = unit.rest, kv_head = attn_divide(head, p.s.share, p.s.per_share).quotient;
+    const bool known = !p.s.starts && !p.s.lengths;
+    if (!known) griddep_wait();
     if (warp == 0) {
-        const AttnTile t = attn_locate(p.s, blockIdx.x / p.s.heads, kAttnRows, p.s.causal);
-        if (lane == 0) work = t;
+        const AttnTile t = attn_locate<kAttnRows>(p.s, unit.quotient, p.s.causal);
+        if (lane == 0) sh.work = t;
     }
+    if (known) griddep_wait();
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
-    const uint32_t tmem = *tmem_slot, t_dp = tmem + 2 * kAttnRows, t_dq = tmem + 3 * kAttnRows;
-    const int len = work.len, first = work.first, q0 = work.tile * kAttnRows;
+    const uint32_t tmem = sh.tmem, t_dp = tmem + 2 * kAttnRows, t_dq = tmem + 3 * kAttnRows;
+    const int len = sh.work.len, first = sh.work.first, q0 = sh.work.tile * kAttnRows;
     const int lo = attn_first_key_tile(p.s, q0), items = len ? attn_end_key_tile(p.s, q0, len) - lo : 0;
     const int last = (len - 1) / kAttnRows, last_rows = len - last * kAttnRows;
     const bool ragged = items && lo + items == last + 1 && last_rows < kAttnRows;     // the last item is the sequence's ragged end
@@ -948,15 +1020,15 @@ attention_bwd_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
         if (warp == 9) {
             if (items && elect_one()) {
                 PipeState ks, vs;
-                attn_load<HD>(sQ, &tmQ, &q_full, head, first + q0);
+                attn_load<HD>(sQ, &tmQ, &sh.q_full, head, first + q0);
                 for (int it = 0; it < items; ++it) {
                     const int row = first + (lo + it) * kAttnRows;
-                    if (!attn_wait(&k_empty[ks.stage], ks.phase ^ 1u, abort_flag)) break;
-                    attn_load<HD>(keys + ks.stage * Cfg::kTile, &tmK, ragged && it + 1 == items ? &ragged_bar : &k_full[ks.stage], kv_head, row);
+                    if (!attn_wait(&sh.k_empty[ks.stage], ks.phase ^ 1u, abort_flag)) break;
+                    attn_load<HD>(keys + ks.stage * Cfg::kTile, &tmK, ragged && it + 1 == items ? &sh.ragged_bar : &sh.k_full[ks.stage], kv_head, row);
                     ks.advance(Cfg::kKeys);
-                    if (it == 0) attn_load<HD>(sdO, &tmdO, &do_full, head, first + q0);
-                    if (!attn_wait(&v_empty[vs.stage], vs.phase ^ 1u, abort_flag)) break;
-                    attn_load<HD>(values + vs.stage * Cfg::kTile, &tmV, &v_full[vs.stage], kv_head, row);
+                    if (it == 0) attn_load<HD>(sdO, &tmdO, &sh.do_full, head, first + q0);
+                    if (!attn_wait(&sh.v_empty[vs.stage], vs.phase ^ 1u, abort_flag)) break;
+                    attn_load<HD>(values + vs.stage * Cfg::kTile, &tmV, &sh.v_full[vs.stage], kv_head, row);
                     vs.advance(Cfg::kValues);
                 }
             }
@@ -968,39 +1040,39 @@ attention_bwd_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
                                key_rows = attn_row_desc(keys), value_desc = attn_column_desc(values);
                 PipeState ks, vs;                         // of the next scores and of the next products
                 const auto scores = [&](int it) {
-                    if (!attn_wait(&k_full[ks.stage], ks.phase, abort_flag)) return false;
+                    if (!attn_wait(&sh.k_full[ks.stage], ks.phase, abort_flag)) return false;
                     tc_fence_after_sync();
                     attn_mma_columns<HD>(tmem + (it & 1) * kAttnRows, q_desc, key_desc + ks.stage * (Cfg::kTile >> 4), steps);
-                    umma_commit(&s_full[it & 1]);
+                    umma_commit(&sh.s_full[it & 1]);
                     ks.advance(Cfg::kKeys);
                     return true;
                 };
                 const auto products = [&](int it) {
-                    if (!attn_wait(&v_full[vs.stage], vs.phase, abort_flag)) return false;
+                    if (!attn_wait(&sh.v_full[vs.stage], vs.phase, abort_flag)) return false;
                     tc_fence_after_sync();
                     attn_mma_columns<HD>(t_dp, do_desc, value_desc + vs.stage * (Cfg::kTile >> 4), steps);
-                    umma_commit(&dp_full[it & 1]);
-                    umma_commit(&v_empty[vs.stage]);
+                    umma_commit(&sh.dp_full[it & 1]);
+                    umma_commit(&sh.v_empty[vs.stage]);
                     vs.advance(Cfg::kValues);
                     return true;
                 };
-                bool ok = attn_wait(&q_full, 0, abort_flag) && scores(0) && attn_wait(&do_full, 0, abort_flag) && products(0) && (items < 2 || scores(1));
+                bool ok = attn_wait(&sh.q_full, 0, abort_flag) && scores(0) && attn_wait(&sh.do_full, 0, abort_flag) && products(0) && (items < 2 || scores(1));
                 for (int it = 0; it < items && ok; ++it) {
                     const int rows = ragged && it + 1 == items ? last_rows : kAttnRows, g = it & 1, stage = it % Cfg::kKeys;
                     const uint32_t t_s = tmem + g * kAttnRows, phase = (it >> 1) & 1;
-                    if (!(ok = attn_wait(&dp_read[g], phase, abort_flag) && (it + 1 >= items || products(it + 1)) && attn_wait(&ds_ready[g], phase, abort_flag)))
+                    if (!(ok = attn_wait(&sh.dp_read[g], phase, abort_flag) && (it + 1 >= items || products(it + 1)) && attn_wait(&sh.ds_ready[g], phase, abort_flag)))
                         break;
                     tc_fence_after_sync();
                     attn_mma_rows(t_dq, t_s, t_s + 64, key_rows + stage * (Cfg::kTile >> 4), idesc, (rows + 15) / 16, it != 0);
-                    umma_commit(it + 1 < items ? &k_empty[stage] : &acc_full);
+                    umma_commit(it + 1 < items ? &sh.k_empty[stage] : &sh.acc_full);
                     if (it + 2 < items) ok = scores(it + 2);
                 }
             }
         } else if (warp == 10 && ragged) {
             const int stage = (items - 1) % Cfg::kKeys;
-            if (warp_wait(&ragged_bar, 0, abort_flag)) {
+            if (warp_wait(&sh.ragged_bar, 0, abort_flag)) {
                 attn_zero_rows<HD>(keys + stage * Cfg::kTile, last_rows);
-                warp_arrive(&k_full[stage]);
+                warp_arrive(&sh.k_full[stage]);
             }
         }
     } else {
@@ -1019,22 +1091,22 @@ attention_bwd_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
             const bool edge = (p.s.causal ? c0 + kAttnRows - 1 > q0 : c0 + kAttnRows > len) || (p.s.window && q0 + kAttnRows - 1 - c0 >= p.s.window);
             const int c_hi = (p.s.causal ? min(i + 1, len) : len) - c0, c_lo = p.s.window ? i - p.s.window + 1 - c0 : 0;
             const uint32_t s_row = tmem + group * kAttnRows + lanes, dp_row = t_dp + lanes, phase = (it >> 1) & 1;
-            if (!(ok = warp_wait(&s_full[group], phase, abort_flag))) break;
+            if (!(ok = warp_wait(&sh.s_full[group], phase, abort_flag))) break;
             tc_fence_after_sync();
             uint32_t v[kAttnRows];
             if (edge) attn_row_powers<true>(s_row, v, p.s.scale, lse, c_lo, c_hi);
             else attn_row_powers<false>(s_row, v, p.s.scale, lse, 0, kAttnRows);
-            if (!(ok = warp_wait(&dp_full[group], phase, abort_flag))) break;
+            if (!(ok = warp_wait(&sh.dp_full[group], phase, abort_flag))) break;
             tc_fence_after_sync();
-            if (edge) attn_row_gradients<true>(dp_row, v, delta, &dp_read[group], c_lo, c_hi);
-            else attn_row_gradients<false>(dp_row, v, delta, &dp_read[group], 0, kAttnRows);
+            if (edge) attn_row_gradients<true>(dp_row, v, delta, &sh.dp_read[group], c_lo, c_hi);
+            else attn_row_gradients<false>(dp_row, v, delta, &sh.dp_read[group], 0, kAttnRows);
             tmem_st_32(s_row, v);
             tmem_st_32(s_row + 64, v + 32);
             tmem_st_wait();
             tc_fence_before_sync();
-            warp_arrive(&ds_ready[group]);
+            warp_arrive(&sh.ds_ready[group]);
         }
-        if (ok && warp_wait(&acc_full, 0, abort_flag)) {
+        if (ok && warp_wait(&sh.acc_full, 0, abort_flag)) {
             tc_fence_after_sync();
             const size_t at = static_cast<size_t>(first) + q0;
             attn_store<HD, HD / 2>(t_dq + lanes, group * HD / 2, p.grad_scale, group ? sdO : sQ,
@@ -1048,6 +1120,21 @@ attention_bwd_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
         tc_fence_after_sync();
         tmem_dealloc(tmem, 512);
     }
+}
+
+// Both in one launch, the keys' blocks first: the queries' fill the machine while the last of these run.
+template <int HD>
+__global__ void __launch_bounds__(kAttnThreads, 1)
+attention_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                     const __grid_constant__ CUtensorMap tmdO, const AttnBwdParams p) {
+    using Cfg = AttnCfg<HD>;
+    // (one object, whose size the host knows: beside seven tiles of 128 columns there are 3 KB)
+    __shared__ AttnBwdShared<HD> sh;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    const int block = static_cast<int>(blockIdx.x) - p.key_blocks;
+    if (block < 0) attn_bwd_keys<HD>(tmQ, tmK, tmV, tmdO, p, blockIdx.x, sh.keys, smem);
+    else attn_bwd_queries<HD>(tmQ, tmK, tmV, tmdO, p, block, sh.queries, smem);
 }
 
 // =====================================================================================
@@ -1130,7 +1217,8 @@ rotary_kernel(const RotaryParams p) {
     }
     __syncthreads();
     constexpr int kPairs = PAIRS ? N / 2 : N;                  // of a task
-    const int turned = p.n / kPairs, rest = p.copy ? (p.head_dim - 2 * p.n) / N : 0, per_head = turned + rest;
+    // neighbouring pairs: eight columns at a time, whose last pairs may be beyond the rotated part
+    const int turned = (p.n + kPairs - 1) / kPairs, rest = p.copy ? (PAIRS ? p.head_dim / N - turned : (p.head_dim - 2 * p.n) / N) : 0, per_head = turned + rest;
     const int per_token = (p.heads[0] + p.heads[1]) * per_head;
     for (int task = threadIdx.x; task < tokens * per_token; task += kRotaryThreads) {
         const int t = task / per_token, in_token = task - t * per_token;
@@ -1143,7 +1231,7 @@ rotary_kernel(const RotaryParams p) {
         const size_t from = row * (which ? p.src_ld[1] : p.src_ld[0]) + head * p.head_dim, to = row * (which ? p.dst_ld[1] : p.dst_ld[0]) + head * p.head_dim;
         float x[N], y[N];
         if (u >= turned) {
-            const int col = 2 * p.n + (u - turned) * N;
+            const int col = PAIRS ? u * N : 2 * p.n + (u - turned) * N;
             load_n<TYPE, N>(src, from + col, x);
             store_n<TYPE, N>(dst, to + col, x);
             continue;
@@ -1153,8 +1241,10 @@ rotary_kernel(const RotaryParams p) {
             load_n<TYPE, N>(src, from + u * N, x);
 #pragma unroll
             for (int i = 0; i < N / 2; ++i) {
-                y[2 * i] = x[2 * i] * c[i] - x[2 * i + 1] * s[i];
-                y[2 * i + 1] = x[2 * i + 1] * c[i] + x[2 * i] * s[i];
+                const bool in = u * kPairs + i < p.n;
+                const float ci = in ? c[i] : 0.0f, si = in ? s[i] : 0.0f;
+                y[2 * i] = in ? x[2 * i] * ci - x[2 * i + 1] * si : x[2 * i];
+                y[2 * i + 1] = in ? x[2 * i + 1] * ci + x[2 * i] * si : x[2 * i + 1];
             }
             store_n<TYPE, N>(dst, to + u * N, y);
         } else {
