@@ -46,10 +46,11 @@ static slope_status_t launch_attn(Kernel kern, long long grid, int threads, int 
     if (!set_smem(kern, smem)) return SLOPE_ERR_CUDA;
     return launch_cluster_ex(kern, static_cast<int>(grid), 1, threads, smem, /*overlap_prologue=*/true, stream, args...);
 }
-template <int HD>
+template <int HD, int TILES>
 static slope_status_t attn_fwd(const AttnFwdParams& p, const CUtensorMap (&tm)[3], cudaStream_t stream) {
-    return launch_attn(attention_fwd_kernel<HD>, attn_units(p.s.b, p.s.sequences, p.s.starts, 2 * kAttnRows) * p.s.heads, kAttnThreads,
-                       AttnCfg<HD>::kSmem, stream, tm[0], tm[1], tm[2], p);
+    using Cfg = AttnFwdCfg<HD, TILES>;
+    return launch_attn(attention_fwd_kernel<HD, TILES>, attn_units(p.s.b, p.s.sequences, p.s.starts, TILES * kAttnRows) * p.s.heads, Cfg::kThreads,
+                       Cfg::kSmem, stream, tm[0], tm[1], tm[2], p);
 }
 template <int HD>
 static slope_status_t attn_bwd(AttnBwdParams p, const AttnDeltaParams& d, const CUtensorMap (&tm)[4], cudaStream_t stream) {
@@ -92,7 +93,15 @@ slope_status_t slope_attention_fwd(const void* Q, int q_ld, const void* K, int k
         return SLOPE_ERR_CUDA;
     const AttnFwdParams p{s, static_cast<uint16_t*>(O), static_cast<float*>(lse), o_ld};
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    return head_dim <= 64 ? attn_fwd<64>(p, tm, stream) : attn_fwd<128>(p, tm, stream);
+    // One tile of queries a block, two blocks on an SM, where few keys make loading and storing a large part of a block's time, or where blocks of two
+    // tiles would not even give every SM one; else two tiles, which share the keys' tiles. Measured, us, one / two:
+    //   heads of 64, 16384 tokens, 16 heads: 16 x 1024 causal 82 / 94, 4 x 4096 causal 206 / 211, 8 x 2048 full 196 / 196, 4 x 4096 full 386 / 372
+    //   heads of 128, 16384 tokens, 8 heads: 64 x 256 causal 36 / 42, 16 x 1024 causal 59 / 60, 8 x 2048 causal 90 / 89, 4 x 4096 full 300 / 282
+    //   1024 tokens alone, causal: 16 heads of 64 16.5 / 19.3, 8 heads of 128 21.7 / 24.9
+    const int reach = p.s.window ? std::min(p.s.window, p.s.part) : causal ? p.s.part / 2 : p.s.part;  // keys of a query, in the mean
+    const bool one = reach <= (head_dim <= 64 ? 2048 : 512) || attn_units(b, sequences, p.s.starts, 2 * kAttnRows) * heads <= info.sm_count;
+    if (head_dim <= 64) return one ? attn_fwd<64, 1>(p, tm, stream) : attn_fwd<64, 2>(p, tm, stream);
+    return one ? attn_fwd<128, 1>(p, tm, stream) : attn_fwd<128, 2>(p, tm, stream);
 }
 
 size_t slope_attention_bwd_workspace_bytes(int b, int heads, int kv_heads, int head_dim) {
@@ -141,15 +150,19 @@ slope_status_t slope_rotary(const void* Q, int q_ld, const void* K, int k_ld, in
         if (!aligned16(p)) return SLOPE_ERR_ALIGNMENT;
     DeviceInfo info;
     if (slope_status_t st = check_arch(info)) return st;
-    RotaryParams p{{Q, K}, {Qr, Kr}, {q_ld, k_ld}, {qr_ld, kr_ld}, {heads, K ? kv_heads : 0}, b, head_dim, rot_dim / 2, 1, Q != Qr, factor,
-                   backward ? -1.0f : 1.0f, static_cast<const int*>(positions), static_cast<const double*>(frequencies)};
-    // Tokens of a block: an angle for every thread, if that leaves four blocks for every SM, or a few tasks for every thread (rotating 20 of 80 columns of
-    // 64 heads, 2039 tokens: 25 tokens a block 116 us, 3 tokens 8)
-    const long long tasks = (static_cast<long long>(heads) + p.heads[1]) * (head_dim / 8) / 2 + 1;
-    const long long most = std::min<long long>({kRotaryThreads / p.n, b / (4ll * info.sm_count), 8 * kRotaryThreads / tasks, 64});
-    p.tokens = static_cast<int>(std::max(1ll, most));
-    // as many values at a time as the rotated part is a multiple of
-    const int wide = interleaved || p.n % 8 == 0 ? 8 : p.n % 4 == 0 ? 4 : p.n % 2 == 0 ? 2 : 1;
+    // as many values at a time as the rotated part is a multiple of; columns behind it are copied where the output is not the input
+    const int n = rot_dim / 2, wide = interleaved || n % 8 == 0 ? 8 : n % 4 == 0 ? 4 : n % 2 == 0 ? 2 : 1;
+    const int turned = interleaved ? (rot_dim + 7) / 8 : n / wide;
+    const int per_head = turned + (Q == Qr ? 0 : interleaved ? head_dim / 8 - turned : (head_dim - rot_dim) / wide);
+    const long long per_token = (static_cast<long long>(heads) + (K ? kv_heads : 0)) * per_head;
+    // Tokens of a block: an angle for every thread, if that leaves four blocks for every SM and a thread two batches of tasks at most (rotating 20 of 80
+    // columns of 64 heads, 2039 tokens: 25 tokens a block 116 us, 3 tokens 25)
+    const long long most = std::min<long long>({kRotaryThreads / n, b / (4ll * info.sm_count), 8 * kRotaryThreads / per_token, 64});
+    const int tokens = static_cast<int>(std::max(1ll, most));
+    if (tokens * per_token > INT_MAX / 2) return SLOPE_ERR_SHAPE;
+    const RotaryParams p{{Q, K}, {Qr, Kr}, {q_ld, k_ld}, {qr_ld, kr_ld}, {heads, K ? kv_heads : 0}, b, head_dim, n, tokens, turned, per_head,
+                         static_cast<int>(per_token), 1.0f / per_head, 1.0f / per_token, factor, backward ? -1.0f : 1.0f,
+                         static_cast<const int*>(positions), static_cast<const double*>(frequencies)};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (type == SLOPE_F32) return interleaved ? launch_rotary<kTypeF32, true>(p, wide, s) : launch_rotary<kTypeF32, false>(p, wide, s);
     return interleaved ? launch_rotary<kTypeBf16, true>(p, wide, s) : launch_rotary<kTypeBf16, false>(p, wide, s);

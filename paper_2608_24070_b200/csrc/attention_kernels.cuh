@@ -210,6 +210,15 @@ union AttnBwdShared {
     AttnKvShared<AttnCfg<HD>::kStages> keys;
     AttnQShared<AttnCfg<HD>::kKeys, AttnCfg<HD>::kValues> queries;
 };
+// The forward pass: TILES tiles of queries a block; with one, two blocks share an SM.
+template <int HD, int TILES>
+struct AttnFwdCfg {
+    static constexpr int kTile = AttnCfg<HD>::kTile, kBlocks = 3 - TILES, kThreads = 128 * (TILES + 1);
+    static constexpr int kStages = TILES == 2 ? AttnCfg<HD>::kStages : HD == 128 ? 2 : 5, kSmem = (TILES + kStages) * kTile + 1024;
+    // registers of a thread that computes / that feeds, out of 168 or 128 a thread at launch
+    static constexpr int kUp = 208, kDown = TILES == 2 ? 88 : 48;
+    static_assert(TILES * kUp + kDown == (TILES + 1) * (TILES == 2 ? 168 : 128), "shares of the launch's registers");
+};
 template <int HD>
 __device__ __forceinline__ void attn_load(uint8_t* tile, const CUtensorMap* tm, uint64_t* bar, int head, int row) {
     mbar_expect_tx(bar, AttnCfg<HD>::kTile);
@@ -365,24 +374,24 @@ struct AttnFwdParams {
     float* lse;
     int o_ld;
 };
-template <int HD>
-__global__ void __launch_bounds__(kAttnThreads, 1)
+template <int HD, int TILES>
+__global__ void __launch_bounds__(AttnFwdCfg<HD, TILES>::kThreads, AttnFwdCfg<HD, TILES>::kBlocks)
 attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                      const AttnFwdParams p) {
-    using Cfg = AttnCfg<HD>;
-    __shared__ uint64_t q_full[2], s_full[2], s_read[2], p_full[2][2], pv_done[2], o_full[2], full_bar[Cfg::kStages], empty_bar[Cfg::kStages], ragged_bar;
+    using Cfg = AttnFwdCfg<HD, TILES>;
+    __shared__ uint64_t q_full[TILES], s_full[TILES], s_read[TILES], p_full[TILES][2], pv_done[TILES], o_full[TILES], full_bar[Cfg::kStages], empty_bar[Cfg::kStages], ragged_bar;
     __shared__ uint32_t tmem_slot[1];
     __shared__ int abort_word;
     __shared__ AttnTile work;
     volatile int* abort_flag = &abort_word;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    uint8_t* ring = smem + 2 * Cfg::kTile;
+    uint8_t* ring = smem + TILES * Cfg::kTile;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = threadIdx.x >> 7;
 
     griddep_launch_dependents();
     if (threadIdx.x == 0) {
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < TILES; ++t) {
             mbar_init(&q_full[t], 1);
             mbar_init(&s_full[t], 1);
             mbar_init(&s_read[t], 4);
@@ -396,8 +405,8 @@ attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         *abort_flag = 0;
         fence_mbar_init();
     }
-    if (warp == 8) {
-        tmem_alloc(tmem_slot, 512);
+    if (warp == 4 * TILES) {
+        tmem_alloc(tmem_slot, 256 * TILES);
         tmem_relinquish();
     }
     const AttnQuotient unit = attn_divide(blockIdx.x, p.s.heads, p.s.per_heads);
@@ -406,7 +415,7 @@ attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
     const bool known = !p.s.starts && !p.s.lengths;
     if (!known) griddep_wait();
     if (warp == 0) {
-        const AttnTile t = attn_locate<2 * kAttnRows>(p.s, unit.quotient, p.s.causal);
+        const AttnTile t = attn_locate<TILES * kAttnRows>(p.s, unit.quotient, p.s.causal);
         if (lane == 0) work = t;
     }
     if (known) griddep_wait();
@@ -417,23 +426,24 @@ attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
     // for these ones to be read only (us, 4 x 4096 tokens, 16 heads: over / apart 384 / 340)
     constexpr bool kApart = HD == 64;
     const uint32_t tmem = *tmem_slot;
-    const auto p_at = [&](int t, int h) { return kApart ? tmem + 3 * kAttnRows + 64 * t + 32 * h : tmem + kAttnRows * t + 64 * h; };
-    const int len = work.len, first = work.first, q0 = work.tile * 2 * kAttnRows;
-    const int tiles = !len ? 0 : len - q0 > kAttnRows ? 2 : 1;
-    // tiles of keys [lo, hi) of the two tiles of queries and of both
-    int lo[2], hi[2];
+    const uint32_t o_at = tmem + TILES * kAttnRows;
+    const auto p_at = [&](int t, int h) { return kApart ? o_at + TILES * HD + 64 * t + 32 * h : tmem + kAttnRows * t + 64 * h; };
+    const int len = work.len, first = work.first, q0 = work.tile * TILES * kAttnRows;
+    const int tiles = !len ? 0 : min(TILES, (len - q0 - 1) / kAttnRows + 1);
+    // tiles of keys [lo, hi) of each tile of queries and of all
+    int lo[TILES], hi[TILES];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < TILES; ++t) {
         lo[t] = attn_first_key_tile(p.s, q0 + t * kAttnRows);
         hi[t] = t < tiles ? attn_end_key_tile(p.s, q0 + t * kAttnRows, len) : lo[t];
     }
-    const int begin = lo[0], end = tiles ? max(hi[0], hi[1]) : begin;
+    const int begin = lo[0], end = tiles ? max(hi[0], hi[TILES - 1]) : begin;
     // the sequence's last tile of keys, if it is not full and among these
     const int last = (len - 1) / kAttnRows, last_rows = len - last * kAttnRows, ragged = last_rows < kAttnRows && end == last + 1 ? last : -1;
 
-    if (group == 2) {
-        registers_down<kAttnRegsDown>();
-        if (warp == 9) {
+    if (group == TILES) {
+        registers_down<Cfg::kDown>();
+        if (warp == 4 * TILES + 1) {
             if (elect_one()) {
                 PipeState ps;
                 bool ok = true;
@@ -448,13 +458,13 @@ attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                     }
                 }
             }
-        } else if (warp == 8) {
+        } else if (warp == 4 * TILES) {
             if (elect_one()) {
                 const int steps = (p.s.head_dim + 15) / 16;
                 PipeState ps;                             // of the next tile of the ring to be waited for
                 const uint32_t idesc = attn_row_idesc(p.s.head_dim);
                 const uint64_t q_desc = attn_column_desc(smem), column_desc = attn_column_desc(ring), row_desc = attn_row_desc(ring);
-                uint32_t phase[2] = {0, 0};
+                uint32_t phase[TILES] = {};
                 bool ok = true;
                 const auto scores = [&](int t, int stage) {
                     attn_mma_columns<HD>(tmem + t * kAttnRows, q_desc + t * (Cfg::kTile >> 4), column_desc + stage * (Cfg::kTile >> 4), steps);
@@ -463,7 +473,7 @@ attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                 // the first scores; behind them each step leaves those of the next
                 if (begin < end && (ok = attn_wait(&full_bar[ps.stage], ps.phase, abort_flag))) {
 #pragma unroll
-                    for (int t = 0; t < 2; ++t) {
+                    for (int t = 0; t < TILES; ++t) {
                         if (t >= tiles || !(ok = ok && attn_wait(&q_full[t], 0, abort_flag))) continue;
                         tc_fence_after_sync();
                         if (lo[t] <= begin && begin < hi[t]) scores(t, ps.stage);
@@ -481,7 +491,7 @@ attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                         ps.advance(Cfg::kStages);
                     }
 #pragma unroll
-                    for (int t = 0; t < 2; ++t) {
+                    for (int t = 0; t < TILES; ++t) {
                         const bool next = lo[t] <= j + 1 && j + 1 < hi[t];
                         if (kApart && next) {
                             if (lo[t] <= j && !(ok = ok && attn_wait(&s_read[t], phase[t], abort_flag))) continue;
@@ -489,7 +499,7 @@ attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                             scores(t, k_stage);
                         }
                         if (lo[t] <= j && j < hi[t]) {
-                            const uint32_t o = tmem + 2 * kAttnRows + t * HD;
+                            const uint32_t o = o_at + t * HD;
                             const uint64_t v = row_desc + v_stage * (Cfg::kTile >> 4);
                             if (!(ok = ok && attn_wait(&p_full[t][0], phase[t], abort_flag))) continue;
                             tc_fence_after_sync();
@@ -508,7 +518,7 @@ attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                     if (j + 1 < end) umma_commit(&empty_bar[k_stage]);
                 }
             }
-        } else if (warp == 10 && ragged >= 0) {
+        } else if (warp == 4 * TILES + 2 && ragged >= 0) {
             const int stage = (2 * (last - begin) + 1) % Cfg::kStages;
             if (warp_wait(&ragged_bar, 0, abort_flag)) {
                 attn_zero_rows<HD>(ring + stage * Cfg::kTile, last_rows);
@@ -516,15 +526,15 @@ attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             }
         }
     } else {
-        registers_up<kAttnRegsUp>();
+        registers_up<Cfg::kUp>();
         const int t = group, row = threadIdx.x & 127, t0 = q0 + t * kAttnRows, i = t0 + row;       // the query's place in its sequence
         const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-        const uint32_t s_row = tmem + lanes + t * kAttnRows, o_row = tmem + lanes + 2 * kAttnRows + t * HD;
+        const uint32_t s_row = tmem + lanes + t * kAttnRows, o_row = o_at + lanes + t * HD;
         float m = -INFINITY, l = 0.0f;
         uint32_t phase = 0;
         bool ok = t < tiles;
         const float by = p.s.scale;
-        const int j_lo = t ? lo[1] : lo[0], j_hi = t ? hi[1] : hi[0];
+        const int j_lo = t ? lo[TILES - 1] : lo[0], j_hi = t ? hi[TILES - 1] : hi[0];
         for (int j = j_lo; j < j_hi; ++j) {
             if (!(ok = warp_wait(&s_full[t], phase, abort_flag))) break;
             phase ^= 1u;
@@ -582,9 +592,9 @@ attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
     }
     if (*abort_flag) drain_after_abort();
     __syncthreads();
-    if (warp == 8) {
+    if (warp == 4 * TILES) {
         tc_fence_after_sync();
-        tmem_dealloc(tmem, 512);
+        tmem_dealloc(tmem, 256 * TILES);
     }
 }
 
@@ -1149,7 +1159,8 @@ struct RotaryParams {
     void* dst[2];
     int src_ld[2], dst_ld[2], heads[2];
     int b, head_dim, n, tokens;           // n: pairs of a head; tokens of a block
-    int copy;                             // columns behind the rotated ones are copied (not where the output is the input)
+    int turned, per_head, per_token;      // tasks of a head that rotate; all of a head's, with those that copy the columns behind; a token's
+    float per_per_head, per_per_token;    // their reciprocals
     float factor, sign;
     const int* positions;
     const double* frequencies;
@@ -1197,14 +1208,43 @@ __device__ __forceinline__ void store_n(void* base, size_t at, const float (&x)[
     }
 }
 constexpr int kRotaryThreads = 256, kRotaryTable = 2048;       // angles of a block
-// A thread takes N values at a time: N pairs' two halves, or N / 2 neighbouring pairs.
+// A thread takes N values at a time: N pairs' two halves, or N / 2 neighbouring pairs; kBatch of these are in flight, the first while the block's
+// angles are formed.  Measured, us, one at a time behind the angles / two / four: 20 of 80 columns of 64 heads turned, 2039 tokens, neighbouring pairs
+// 17.2 / 9.2 / 10.2, halves 41.8 / 20.8 / 23.9; all of 64 heads of 128, 16384 tokens, bf16, halves 84.7 / 83.2 / 100; fp32, where a task of eight
+// has four loads of its own and goes alone, 40 heads of 128, 8191 tokens, 55.1 / 55.6 / -, one in flight 54.9.
 template <int TYPE, bool PAIRS, int N>
 __global__ void __launch_bounds__(kRotaryThreads)
 rotary_kernel(const RotaryParams p) {
     __shared__ float cosine[kRotaryTable], sine[kRotaryTable];
     griddep_launch_dependents();
     griddep_wait();
-    const int token0 = blockIdx.x * p.tokens, tokens = min(p.tokens, p.b - token0);
+    const int token0 = blockIdx.x * p.tokens, tokens = min(p.tokens, p.b - token0), tasks = tokens * p.per_token;
+    constexpr int kBatch = !PAIRS && N == 8 && TYPE == kTypeF32 ? 1 : 2;
+    constexpr int kPairs = PAIRS ? N / 2 : N;                  // of a task
+    float x[kBatch][N], z[kBatch][N];
+    void* row[kBatch];                                         // of the output, at the task's head
+    int angle[kBatch], column[kBatch];                         // angle: the first one's place, -1 in a task that copies
+    const auto fetch = [&](int first) {
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            // (past the end: the last task once more, which is not stored)
+            const AttnQuotient token = attn_divide(min(first + j * kRotaryThreads, tasks - 1), p.per_token, p.per_per_token);
+            const AttnQuotient head = attn_divide(token.rest, p.per_head, p.per_per_head);
+            const bool which = head.quotient >= p.heads[0];
+            const int h = which ? head.quotient - p.heads[0] : head.quotient, u = head.rest;
+            const size_t at = static_cast<size_t>(token0 + token.quotient);
+            constexpr int kBytes = TYPE == kTypeF32 ? 4 : 2;
+            const size_t from = at * (which ? p.src_ld[1] : p.src_ld[0]) + h * p.head_dim, to = at * (which ? p.dst_ld[1] : p.dst_ld[0]) + h * p.head_dim;
+            const void* src = which ? p.src[1] : p.src[0];
+            row[j] = static_cast<uint8_t*>(which ? p.dst[1] : p.dst[0]) + to * kBytes;
+            const bool turns = u < p.turned;
+            angle[j] = turns ? token.quotient * p.n + u * kPairs : -1;
+            column[j] = PAIRS || turns ? u * N : 2 * p.n + (u - p.turned) * N;
+            load_n<TYPE, N>(src, from + column[j], x[j]);
+            if (!PAIRS) load_n<TYPE, N>(src, from + column[j] + (turns ? p.n : 0), z[j]);
+        }
+    };
+    fetch(threadIdx.x);
     for (int i = threadIdx.x; i < tokens * p.n; i += kRotaryThreads) {
         const int t = i / p.n;
         const uint2 f = ld_v2(p.frequencies + (i - t * p.n));
@@ -1216,48 +1256,34 @@ rotary_kernel(const RotaryParams p) {
         sine[i] = s * p.factor * p.sign;
     }
     __syncthreads();
-    constexpr int kPairs = PAIRS ? N / 2 : N;                  // of a task
-    // neighbouring pairs: eight columns at a time, whose last pairs may be beyond the rotated part
-    const int turned = (p.n + kPairs - 1) / kPairs, rest = p.copy ? (PAIRS ? p.head_dim / N - turned : (p.head_dim - 2 * p.n) / N) : 0, per_head = turned + rest;
-    const int per_token = (p.heads[0] + p.heads[1]) * per_head;
-    for (int task = threadIdx.x; task < tokens * per_token; task += kRotaryThreads) {
-        const int t = task / per_token, in_token = task - t * per_token;
-        int head = in_token / per_head;
-        const int u = in_token - head * per_head, which = head >= p.heads[0];
-        if (which) head -= p.heads[0];
-        const size_t row = static_cast<size_t>(token0 + t);
-        const void* src = which ? p.src[1] : p.src[0];
-        void* dst = which ? p.dst[1] : p.dst[0];
-        const size_t from = row * (which ? p.src_ld[1] : p.src_ld[0]) + head * p.head_dim, to = row * (which ? p.dst_ld[1] : p.dst_ld[0]) + head * p.head_dim;
-        float x[N], y[N];
-        if (u >= turned) {
-            const int col = PAIRS ? u * N : 2 * p.n + (u - turned) * N;
-            load_n<TYPE, N>(src, from + col, x);
-            store_n<TYPE, N>(dst, to + col, x);
-            continue;
-        }
-        const float *c = cosine + t * p.n + u * kPairs, *s = sine + t * p.n + u * kPairs;
-        if (PAIRS) {
-            load_n<TYPE, N>(src, from + u * N, x);
+    for (int first = threadIdx.x; first < tasks; first += kBatch * kRotaryThreads) {
+        if (first >= kRotaryThreads) fetch(first);
 #pragma unroll
-            for (int i = 0; i < N / 2; ++i) {
-                const bool in = u * kPairs + i < p.n;
-                const float ci = in ? c[i] : 0.0f, si = in ? s[i] : 0.0f;
-                y[2 * i] = in ? x[2 * i] * ci - x[2 * i + 1] * si : x[2 * i];
-                y[2 * i + 1] = in ? x[2 * i + 1] * ci + x[2 * i] * si : x[2 * i + 1];
-            }
-            store_n<TYPE, N>(dst, to + u * N, y);
-        } else {
-            float z[N];
-            load_n<TYPE, N>(src, from + u * N, x);
-            load_n<TYPE, N>(src, from + p.n + u * N, z);
+        for (int j = 0; j < kBatch; ++j) {
+            if (first + j * kRotaryThreads >= tasks) break;
+            if (angle[j] >= 0) {
+                const float *c = cosine + angle[j], *s = sine + angle[j];
+                if (PAIRS) {
+                    // the last of the eight columns may be behind the rotated part
+                    const int in = p.n - (column[j] >> 1);
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                y[i] = x[i] * c[i] - z[i] * s[i];
-                z[i] = z[i] * c[i] + x[i] * s[i];
+                    for (int i = 0; i < N / 2; ++i) {
+                        if (i >= in) break;
+                        const float u = x[j][2 * i], v = x[j][2 * i + 1];
+                        x[j][2 * i] = u * c[i] - v * s[i];
+                        x[j][2 * i + 1] = v * c[i] + u * s[i];
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        const float u = x[j][i], v = z[j][i];
+                        x[j][i] = u * c[i] - v * s[i];
+                        z[j][i] = v * c[i] + u * s[i];
+                    }
+                    store_n<TYPE, N>(row[j], column[j] + p.n, z[j]);
+                }
             }
-            store_n<TYPE, N>(dst, to + u * N, y);
-            store_n<TYPE, N>(dst, to + p.n + u * N, z);
+            store_n<TYPE, N>(row[j], column[j], x[j]);
         }
     }
 }

@@ -289,3 +289,35 @@ def test_long_sequence(B):
     hd, n = 128, 5000
     Q, K, V, dO = tensors(n, 2, 1, hd, 23)
     compare(run(B, Q, K, V, dO, hd), Q, K, V, dO, hd, [(0, n)])
+
+
+@pytest.mark.parametrize("hd,heads,kv,lengths,causal,window", [
+    (64, 8, 4, [5000, 300, 1000], False, 0), (64, 4, 2, [8000, 300, 4000], True, 0),
+    (128, 12, 6, [1000, 1, 0, 900, 2040], False, 0), (128, 12, 6, [1000, 1, 2300, 900, 2040], True, 0), (128, 12, 6, [600] * 6, True, 520),
+])
+def test_blocks_of_two_tiles(B, hd, heads, kv, lengths, causal, window):
+    """Many keys to a query and blocks enough for every SM: the forward pass takes 256 queries to a block."""
+    import torch
+
+    starts = [0]
+    for n in lengths:
+        starts.append(starts[-1] + n)
+    Q, K, V, dO = tensors(starts[-1], heads, kv, hd, 24)
+    got = run(B, Q, K, V, dO, hd, starts=torch.tensor(starts, dtype=torch.int32, device="cuda"), causal=causal, window=window)
+    compare(got, Q, K, V, dO, hd, list(zip(starts, lengths)), causal, window)
+
+
+@pytest.mark.parametrize("lengths", [[600, 0, 1, 599, 256, 257], [255, 129, 128, 127, 512, 513]])
+def test_blocks_of_two_tiles_in_padded_batches(B, lengths):
+    import torch
+
+    hd, heads = 128, 9
+    clean = tensors(1100 * len(lengths), heads, heads, hd, 25)
+    inside = torch.zeros(1100 * len(lengths), dtype=torch.bool, device="cuda")
+    for i, n in enumerate(lengths):
+        inside[1100 * i:1100 * i + n] = True
+    for causal in (True, False):
+        batch = {"sequences": len(lengths), "lengths": torch.tensor(lengths, dtype=torch.int32, device="cuda"), "causal": causal}
+        for bad in (0.0, float("nan")):
+            Q, K, V, dO = (x.masked_fill(~inside[:, None], bad) for x in clean)
+            compare(run(B, Q, K, V, dO, hd, **batch), Q, K, V, dO, hd, [(1100 * i, n) for i, n in enumerate(lengths)], causal)
