@@ -99,8 +99,9 @@ struct AttnTile {
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 constexpr int kAttnRows = 128;            // rows of a tile of queries or keys
 constexpr int kAttnThreads = 384;         // two groups of four warps that compute, one that feeds them
-// registers of a thread that computes / that feeds; with 168 at launch the three groups come to 384 x 168
-constexpr int kAttnRegsUp = 208, kAttnRegsDown = 88;
+// backward: registers of a thread that computes / that feeds; with 168 at launch the three groups come to 384 x 168.  (us, 4 x 2048 tokens, 40 heads of
+// 128, causal: 200 768, 208 747, 216 740, 224 744; what feeds has too few then)
+constexpr int kAttnRegsUp = 216, kAttnRegsDown = 72;
 static_assert(2 * kAttnRegsUp + kAttnRegsDown == 3 * 168, "shares of the launch's registers");
 
 // x / d and what is left, x >= 0, with the reciprocal at hand (a division takes 100 clocks, and a block has four in front of its first load).
@@ -187,12 +188,17 @@ struct AttnCfg {
     static constexpr int kKeys = HD == 128 ? 3 : 4, kValues = kStages - kKeys;
 };
 // What a block of dK and dV has beside its tiles ...
-template <int STAGES>
+template <int HD, int STAGES>
 struct alignas(128) AttnKvShared {
+    static constexpr int kLse = HD == 64 ? 2 : 1;
     uint4 minus_d[kAttnRows];             // of a tile's queries: -D / 2 as a sum of three bf16 values, zeros behind them
     uint4 ones[8];                        // eight rows of three ones
-    float lse[kAttnRows];                 // in powers of two
-    uint64_t k_full, v_full, acc_full, s_full[2], s_read[2], dp_full[2], pairs_full[2][2], powers_done, d_full, full[STAGES], empty[STAGES], ragged[STAGES];
+    float lse[kLse][kAttnRows];           // in powers of two; with two places (which 64 columns leave room for) the groups' powers need not wait for one another:
+                                          // 4 x 4096 tokens, 16 heads, full, 1160 -> 1110 us
+    // completed by one arrival, by two (the scores, and what belongs to their queries), by a group's four warps
+    uint64_t k_full, v_full, acc_full, d_full, dp_full[2], full[STAGES], empty[STAGES], ragged[STAGES];
+    uint64_t s_full[2];
+    uint64_t s_read[2], pairs_full[2][2], powers_done[kLse];
     uint32_t tmem;
     int abort_word;
     AttnTile work;
@@ -200,14 +206,16 @@ struct alignas(128) AttnKvShared {
 // ... and that of dQ
 template <int KEYS, int VALUES>
 struct alignas(128) AttnQShared {
-    uint64_t q_full, do_full, s_full[2], dp_full[2], dp_read[2], ds_ready[2], acc_full, ragged_bar, k_full[KEYS], k_empty[KEYS], v_full[VALUES], v_empty[VALUES];
+    // completed by one arrival, by a group's four warps
+    uint64_t q_full, do_full, s_full[2], dp_full[2], acc_full, ragged_bar, k_full[KEYS], k_empty[KEYS], v_full[VALUES], v_empty[VALUES];
+    uint64_t dp_read[2], ds_ready[2];
     uint32_t tmem;
     int abort_word;
     AttnTile work;
 };
 template <int HD>
 union AttnBwdShared {
-    AttnKvShared<AttnCfg<HD>::kStages> keys;
+    AttnKvShared<HD, AttnCfg<HD>::kStages> keys;
     AttnQShared<AttnCfg<HD>::kKeys, AttnCfg<HD>::kValues> queries;
 };
 // The forward pass: TILES tiles of queries a block; with one, two blocks share an SM.
@@ -269,6 +277,10 @@ __device__ __forceinline__ uint32_t attn_row_idesc(int head_dim) { return make_i
 __device__ __forceinline__ uint32_t attn_bits(int lo, int hi) {
     const uint32_t below_hi = hi >= 32 ? 0xFFFFFFFFu : hi <= 0 ? 0u : (1u << hi) - 1u, below_lo = lo >= 32 ? 0xFFFFFFFFu : lo <= 0 ? 0u : (1u << lo) - 1u;
     return below_hi & ~below_lo;
+}
+// Barriers [begin, end), by a warp
+__device__ __forceinline__ void attn_barriers(uint64_t* begin, uint64_t* end, uint32_t count) {
+    for (uint64_t* bar = begin + (threadIdx.x & 31); bar < end; bar += 32) mbar_init(bar, count);
 }
 // Rows [valid, 16-multiple) of a tile to zero: they belong to other sequences or to none, and what stands there may be an infinity or a NaN,
 // which a probability of zero does not take out of a product.  Such a tile's copies complete on a barrier of its own, for one warp that zeroes the
@@ -719,28 +731,15 @@ __device__ __forceinline__ uint4 attn_split(float x) {
 // Warp 11: the MMAs of S; 8: the others; 9: loads; 10: lse and D, zeros behind the sequence's last row.
 template <int HD>
 __device__ __forceinline__ void attn_bwd_keys(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmdO,
-                                              const AttnBwdParams& p, int block, AttnKvShared<AttnCfg<HD>::kStages>& sh, uint8_t* smem) {
+                                              const AttnBwdParams& p, int block, AttnKvShared<HD, AttnCfg<HD>::kStages>& sh, uint8_t* smem) {
     using Cfg = AttnCfg<HD>;
     volatile int* abort_flag = &sh.abort_word;
     uint8_t *sK = smem, *sV = smem + Cfg::kTile, *ring = smem + 2 * Cfg::kTile;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = threadIdx.x >> 7;
 
     griddep_launch_dependents();
-    if (threadIdx.x == 0) {
-        for (uint64_t* bar : {&sh.k_full, &sh.v_full, &sh.acc_full, &sh.d_full, &sh.dp_full[0], &sh.dp_full[1]}) mbar_init(bar, 1);
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(&sh.s_full[i], 2);                    // the scores, and what belongs to their queries
-            mbar_init(&sh.s_read[i], 4);
-            mbar_init(&sh.pairs_full[i][0], 4);
-            mbar_init(&sh.pairs_full[i][1], 4);
-        }
-        mbar_init(&sh.powers_done, 4);
-        for (int i = 0; i < Cfg::kStages; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); mbar_init(&sh.ragged[i], 1); }
-        *abort_flag = 0;
-        fence_mbar_init();
-    }
-    if (threadIdx.x >= 32 && threadIdx.x < 40) {
-        sh.ones[threadIdx.x - 32] = make_uint4(0x3F803F80u, 0x00003F80u, 0u, 0u);
+    if (threadIdx.x < 8) {
+        sh.ones[threadIdx.x] = make_uint4(0x3F803F80u, 0x00003F80u, 0u, 0u);
         fence_proxy_async_smem();
     }
     if (warp == 8) {
@@ -749,13 +748,28 @@ __device__ __forceinline__ void attn_bwd_keys(const CUtensorMap& tmQ, const CUte
     }
     const AttnQuotient unit = attn_divide(block, p.s.kv_heads, p.s.per_kv_heads);
     const int kv_head = unit.rest, share = p.s.share;
-    const bool known = !p.s.starts && !p.s.lengths;
-    if (!known) griddep_wait();
-    if (warp == 0) {
+    // The warp that loads sets the barriers up, a lane each, and has the first item's tiles on their way before the others go on.
+    if (warp == 9) {
+        attn_barriers(&sh.k_full, sh.s_full, 1);
+        attn_barriers(sh.s_full, sh.s_read, 2);
+        attn_barriers(sh.s_read, reinterpret_cast<uint64_t*>(&sh.tmem), 4);
+        if (lane == 0) *abort_flag = 0;
+        fence_mbar_init();
+        griddep_wait();
         const AttnTile t = attn_locate<kAttnRows>(p.s, unit.quotient, false);
         if (lane == 0) sh.work = t;
+        __syncwarp();
+        if (t.len && elect_one()) {
+            const int k0 = t.tile * kAttnRows, tile = attn_first_query_tile(p.s, k0);
+            uint64_t* bars = (tile + 1) * kAttnRows > t.len ? sh.ragged : sh.full;
+            attn_load<HD>(sK, &tmK, &sh.k_full, kv_head, t.first + k0);
+            attn_load<HD>(ring, &tmQ, &bars[0], kv_head * share, t.first + tile * kAttnRows);
+            attn_load<HD>(sV, &tmV, &sh.v_full, kv_head, t.first + k0);
+            attn_load<HD>(ring + Cfg::kTile, &tmdO, &bars[1], kv_head * share, t.first + tile * kAttnRows);
+        }
+        __syncwarp();
     }
-    if (known) griddep_wait();
+    griddep_wait();
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
@@ -775,15 +789,13 @@ __device__ __forceinline__ void attn_bwd_keys(const CUtensorMap& tmQ, const CUte
             if (items && elect_one()) {
                 PipeState ps;
                 bool ok = true;
-                attn_load<HD>(sK, &tmK, &sh.k_full, kv_head, first + k0);
                 for (int it = 0, tile = lo, head = kv_head * share; it < items && ok; ++it) {
                     uint64_t* bars = rows_of(tile) < kAttnRows ? sh.ragged : sh.full;
 #pragma unroll
                     for (int g = 0; g < 2; ++g) {
                         if (!attn_wait(&sh.empty[ps.stage], ps.phase ^ 1u, abort_flag)) { ok = false; break; }
-                        attn_load<HD>(ring + ps.stage * Cfg::kTile, g ? &tmdO : &tmQ, &bars[ps.stage], head, first + tile * kAttnRows);
+                        if (it) attn_load<HD>(ring + ps.stage * Cfg::kTile, g ? &tmdO : &tmQ, &bars[ps.stage], head, first + tile * kAttnRows);
                         ps.advance(Cfg::kStages);
-                        if (it == 0 && g == 0) attn_load<HD>(sV, &tmV, &sh.v_full, kv_head, first + k0);
                     }
                     if (++tile == hi) { tile = lo; ++head; }
                 }
@@ -871,10 +883,11 @@ __device__ __forceinline__ void attn_bwd_keys(const CUtensorMap& tmQ, const CUte
                     }
                     if (!ok) break;
                 }
-                // the last tile's powers of two are done, and its dP
-                if (it && !warp_wait(&sh.powers_done, (it - 1) & 1, abort_flag)) break;
+                // the powers of two of the tile that had the place are done, and the last tile's dP
+                constexpr int kLse = sh.kLse;
+                if (it >= kLse && !warp_wait(&sh.powers_done[it % kLse], (it / kLse - 1) & 1, abort_flag)) break;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) sh.lse[lane + 32 * k] = __uint_as_float(e[k]) * kLog2e;
+                for (int k = 0; k < 4; ++k) sh.lse[it % kLse][lane + 32 * k] = __uint_as_float(e[k]) * kLog2e;
                 warp_arrive(&sh.s_full[it & 1]);
                 if (it && !warp_wait(&sh.dp_full[(it - 1) & 1], ((it - 1) >> 1) & 1, abort_flag)) break;
 #pragma unroll
@@ -909,9 +922,9 @@ __device__ __forceinline__ void attn_bwd_keys(const CUtensorMap& tmQ, const CUte
             tie_32(v + 96);
             tc_fence_before_sync();
             warp_arrive(&sh.s_read[group]);
-            if (edge) attn_column_powers<true>(v, p.s.scale, smem_u32(sh.lse), c_lo, c_hi);
-            else attn_column_powers<false>(v, p.s.scale, smem_u32(sh.lse), 0, kAttnRows);
-            warp_arrive(&sh.powers_done);
+            if (edge) attn_column_powers<true>(v, p.s.scale, smem_u32(sh.lse[group % sh.kLse]), c_lo, c_hi);
+            else attn_column_powers<false>(v, p.s.scale, smem_u32(sh.lse[group % sh.kLse]), 0, kAttnRows);
+            warp_arrive(&sh.powers_done[group % sh.kLse]);
             if (!(ok = warp_wait(&sh.dp_full[group], phase, abort_flag))) break;
             tc_fence_after_sync();
             if (edge) attn_column_pairs<true>(dp_row, v, sh.pairs_full[group], c_lo, c_hi);
@@ -995,27 +1008,32 @@ __device__ __forceinline__ void attn_bwd_queries(const CUtensorMap& tmQ, const C
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = threadIdx.x >> 7;
 
     griddep_launch_dependents();
-    if (threadIdx.x == 0) {
-        for (uint64_t* bar : {&sh.q_full, &sh.do_full, &sh.s_full[0], &sh.s_full[1], &sh.dp_full[0], &sh.dp_full[1], &sh.acc_full, &sh.ragged_bar}) mbar_init(bar, 1);
-        for (uint64_t* bar : {&sh.dp_read[0], &sh.dp_read[1], &sh.ds_ready[0], &sh.ds_ready[1]}) mbar_init(bar, 4);
-        for (int i = 0; i < Cfg::kKeys; ++i) { mbar_init(&sh.k_full[i], 1); mbar_init(&sh.k_empty[i], 1); }
-        for (int i = 0; i < Cfg::kValues; ++i) { mbar_init(&sh.v_full[i], 1); mbar_init(&sh.v_empty[i], 1); }
-        *abort_flag = 0;
-        fence_mbar_init();
-    }
     if (warp == 8) {
         tmem_alloc(&sh.tmem, 512);
         tmem_relinquish();
     }
     const AttnQuotient unit = attn_divide(block, p.s.heads, p.s.per_heads);
     const int head = unit.rest, kv_head = attn_divide(head, p.s.share, p.s.per_share).quotient;
-    const bool known = !p.s.starts && !p.s.lengths;
-    if (!known) griddep_wait();
-    if (warp == 0) {
+    if (warp == 9) {
+        attn_barriers(&sh.q_full, sh.dp_read, 1);
+        attn_barriers(sh.dp_read, reinterpret_cast<uint64_t*>(&sh.tmem), 4);
+        if (lane == 0) *abort_flag = 0;
+        fence_mbar_init();
+        griddep_wait();
         const AttnTile t = attn_locate<kAttnRows>(p.s, unit.quotient, p.s.causal);
         if (lane == 0) sh.work = t;
+        __syncwarp();
+        if (t.len && elect_one()) {
+            const int q0 = t.tile * kAttnRows, c0 = attn_first_key_tile(p.s, q0) * kAttnRows;
+            attn_load<HD>(sQ, &tmQ, &sh.q_full, head, t.first + q0);
+            // (ragged: the sequence's end, and with it the only item)
+            attn_load<HD>(keys, &tmK, c0 + kAttnRows > t.len ? &sh.ragged_bar : &sh.k_full[0], kv_head, t.first + c0);
+            attn_load<HD>(sdO, &tmdO, &sh.do_full, head, t.first + q0);
+            attn_load<HD>(values, &tmV, &sh.v_full[0], kv_head, t.first + c0);
+        }
+        __syncwarp();
     }
-    if (known) griddep_wait();
+    griddep_wait();
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
@@ -1030,13 +1048,13 @@ __device__ __forceinline__ void attn_bwd_queries(const CUtensorMap& tmQ, const C
         if (warp == 9) {
             if (items && elect_one()) {
                 PipeState ks, vs;
-                attn_load<HD>(sQ, &tmQ, &sh.q_full, head, first + q0);
-                for (int it = 0; it < items; ++it) {
+                ks.advance(Cfg::kKeys);
+                vs.advance(Cfg::kValues);
+                for (int it = 1; it < items; ++it) {
                     const int row = first + (lo + it) * kAttnRows;
                     if (!attn_wait(&sh.k_empty[ks.stage], ks.phase ^ 1u, abort_flag)) break;
                     attn_load<HD>(keys + ks.stage * Cfg::kTile, &tmK, ragged && it + 1 == items ? &sh.ragged_bar : &sh.k_full[ks.stage], kv_head, row);
                     ks.advance(Cfg::kKeys);
-                    if (it == 0) attn_load<HD>(sdO, &tmdO, &sh.do_full, head, first + q0);
                     if (!attn_wait(&sh.v_empty[vs.stage], vs.phase ^ 1u, abort_flag)) break;
                     attn_load<HD>(values + vs.stage * Cfg::kTile, &tmV, &sh.v_full[vs.stage], kv_head, row);
                     vs.advance(Cfg::kValues);
