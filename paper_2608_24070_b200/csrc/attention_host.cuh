@@ -33,7 +33,7 @@ static long long attn_units(int b, int sequences, bool starts, int rows) {
 }
 static slope_status_t attn_batch(AttnShape* s, int b, int heads, int kv_heads, int head_dim, int sequences, const void* starts, const void* lengths,
                                  int causal, int window, float scale) {
-    if (!(scale > 0.0f && scale <= FLT_MAX) || window < 0 || (window && !causal)) return SLOPE_ERR_INVALID_ARG;
+    if (!(scale > 0.0f && scale * kLog2e <= FLT_MAX) || window < 0 || (window && !causal)) return SLOPE_ERR_INVALID_ARG;
     if (!heads_ok(b, heads, kv_heads, head_dim) || sequences < 1 || (!starts && b % sequences != 0)) return SLOPE_ERR_SHAPE;
     if (attn_units(b, sequences, starts, kAttnRows) * (heads + kv_heads) > INT_MAX) return SLOPE_ERR_SHAPE;
     *s = AttnShape{b, heads, kv_heads, head_dim, sequences, static_cast<const int*>(starts), static_cast<const int*>(lengths), causal != 0,

@@ -100,7 +100,7 @@ constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 constexpr int kAttnRows = 128;            // rows of a tile of queries or keys
 constexpr int kAttnThreads = 384;         // two groups of four warps that compute, one that feeds them
 // backward: registers of a thread that computes / that feeds; with 168 at launch the three groups come to 384 x 168.  (us, 4 x 2048 tokens, 40 heads of
-// 128, causal: 200 768, 208 747, 216 740, 224 744; what feeds has too few then)
+// 128, causal: 200 768, 208 747, 216 740; 224, where the warps that feed run out of theirs, 744)
 constexpr int kAttnRegsUp = 216, kAttnRegsDown = 72;
 static_assert(2 * kAttnRegsUp + kAttnRegsDown == 3 * 168, "shares of the launch's registers");
 
@@ -631,21 +631,31 @@ attention_delta_kernel(const AttnDeltaParams p) {
     griddep_wait();
     const int row0 = (blockIdx.x / ((p.heads + 7) / 8)) * 32, head0 = (blockIdx.x % ((p.heads + 7) / 8)) * 8;
     const int part = threadIdx.x % kLanes, col = 8 * part;
-#pragma unroll 4
-    for (int i = threadIdx.x / kLanes; i < 256; i += kAtOnce) {
-        const int r = i >> 3, h = i & 7, row = row0 + r;
-        float sum = 0.0f;
-        if (row < p.b && head0 + h < p.heads && col < p.head_dim) {
-            const size_t at = (head0 + h) * p.head_dim + col;
-            const V8 a = from_bf16(ld_v4(p.O + static_cast<size_t>(row) * p.o_ld + at)), g = from_bf16(ld_v4(p.dO + static_cast<size_t>(row) * p.do_ld + at));
-            Pair s = mul2(a.p[0], g.p[0]);
+    constexpr int kBatch = 4;
+    for (int i0 = threadIdx.x / kLanes; i0 < 256; i0 += kBatch * kAtOnce) {
+        uint4 a[kBatch], g[kBatch];
 #pragma unroll
-            for (int k = 1; k < 4; ++k) s = fma2(a.p[k], g.p[k], s);
-            sum = low(s) + high(s);
+        for (int j = 0; j < kBatch; ++j) {
+            const int i = i0 + j * kAtOnce, row = row0 + (i >> 3), head = head0 + (i & 7);
+            a[j] = g[j] = make_uint4(0u, 0u, 0u, 0u);
+            if (row < p.b && head < p.heads && col < p.head_dim) {
+                const size_t at = static_cast<size_t>(head) * p.head_dim + col;
+                a[j] = ld_v4(p.O + static_cast<size_t>(row) * p.o_ld + at);
+                g[j] = ld_v4(p.dO + static_cast<size_t>(row) * p.do_ld + at);
+            }
         }
 #pragma unroll
-        for (int d = kLanes / 2; d > 0; d /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-        if (part == 0) out[h][r] = sum;
+        for (int j = 0; j < kBatch; ++j) {
+            const V8 x = from_bf16(a[j]), y = from_bf16(g[j]);
+            Pair s = mul2(x.p[0], y.p[0]);
+#pragma unroll
+            for (int k = 1; k < 4; ++k) s = fma2(x.p[k], y.p[k], s);
+            float sum = low(s) + high(s);
+#pragma unroll
+            for (int d = kLanes / 2; d > 0; d /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+            const int i = i0 + j * kAtOnce;
+            if (part == 0) out[i & 7][i >> 3] = sum;
+        }
     }
     __syncthreads();
     const int h = threadIdx.x >> 5, r = threadIdx.x & 31;

@@ -248,7 +248,7 @@ static slope_status_t launch_result() {
 
 // Opt in to more than 48 KB of dynamic shared memory.  The attribute belongs to the kernel in
 // the current device's context; every host thread remembers which (kernel, device) pairs it has
-// already set (a process-wide flag would be wrong for a second device).  The table has room for all 215 kernels on eight
+// already set (a process-wide flag would be wrong for a second device).  The table has room for all 221 kernels on eight
 // devices, found by hash: with 64 places for the kernels of a signature, of which the layer norm's backward pass has 96, a call to
 // one without a place made two more calls to the runtime each time (0.1 ... 0.2 us of 3).
 static bool set_smem(const void* kernel, int bytes) {

@@ -49,7 +49,7 @@ def test_attention_refusals(lib, a):
     for call in (fwd, bwd):
         for name in ("Q", "K", "V", "O"):
             assert call(**{name: None}) == 1 and call(**{name: a + 8}) == 3, name
-        for scale in (0.0, -1.0, math.inf, math.nan):
+        for scale in (0.0, -1.0, math.inf, math.nan, 3e38):              # (the last is finite, but not in powers of two)
             assert call(scale=scale) == 1
         assert call(window=-1) == 1 and call(window=5, causal=0) == 1
         assert call(b=0) == 2 and call(b=255) == 2 and call(b=(1 << 30) + 2) == 2 and call(sequences=0) == 2

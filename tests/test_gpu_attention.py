@@ -321,3 +321,34 @@ def test_blocks_of_two_tiles_in_padded_batches(B, lengths):
         for bad in (0.0, float("nan")):
             Q, K, V, dO = (x.masked_fill(~inside[:, None], bad) for x in clean)
             compare(run(B, Q, K, V, dO, hd, **batch), Q, K, V, dO, hd, [(1100 * i, n) for i, n in enumerate(lengths)], causal)
+
+
+def test_nothing_to_do(B):
+    """Sequences that are all empty: the call returns, and nothing is written."""
+    import torch
+
+    for hd in (64, 128):
+        Q, K, V, dO = tensors(600, 2, 1, hd, 26)
+        for batch in ({"sequences": 2, "lengths": torch.zeros(2, dtype=torch.int32, device="cuda")},
+                      {"starts": torch.full((6,), 300, dtype=torch.int32, device="cuda")}):
+            for name, x in run(B, Q, K, V, dO, hd, **batch).items():
+                assert (x == 7).all(), name
+
+
+@pytest.mark.parametrize("hd,heads,n", [(64, 16, 1024), (128, 40, 512)])
+def test_more_blocks_than_fit_at_once(B, hd, heads, n):
+    """Several times as many blocks as the device holds, on two streams at once: every sequence as if it were alone."""
+    import torch
+
+    x = tensors(4 * n, heads, heads // 4, hd, 27)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    a = run(B, *x, hd, sequences=4)
+    with torch.cuda.stream(side):
+        b = run(B, *x, hd, sequences=4)
+    torch.cuda.synchronize()
+    for name in a:
+        assert torch.equal(a[name], b[name]), name
+    Q, K, V, dO = (t[2 * n:3 * n] for t in x)
+    got = {name: t[:, 2 * n:3 * n] if name == "lse" else t[2 * n:3 * n] for name, t in a.items()}
+    compare(got, Q, K, V, dO, hd, [(0, n)])
