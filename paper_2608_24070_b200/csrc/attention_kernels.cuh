@@ -391,7 +391,15 @@ __global__ void __launch_bounds__(AttnFwdCfg<HD, TILES>::kThreads, AttnFwdCfg<HD
 attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                      const AttnFwdParams p) {
     using Cfg = AttnFwdCfg<HD, TILES>;
-    __shared__ uint64_t q_full[TILES], s_full[TILES], s_read[TILES], p_full[TILES][2], pv_done[TILES], o_full[TILES], full_bar[Cfg::kStages], empty_bar[Cfg::kStages], ragged_bar;
+    // barriers completed by one arrival, by a group's four warps
+    __shared__ struct {
+        uint64_t q_full[TILES], s_full[TILES], pv_done[TILES], o_full[TILES], full_bar[Cfg::kStages], empty_bar[Cfg::kStages], ragged_bar;
+        uint64_t s_read[TILES], p_full[TILES][2], end[1];
+    } sh;
+    auto &q_full = sh.q_full, &s_full = sh.s_full, &pv_done = sh.pv_done, &o_full = sh.o_full, &s_read = sh.s_read;
+    auto &full_bar = sh.full_bar, &empty_bar = sh.empty_bar;
+    auto& p_full = sh.p_full;
+    uint64_t& ragged_bar = sh.ragged_bar;
     __shared__ uint32_t tmem_slot[1];
     __shared__ int abort_word;
     __shared__ AttnTile work;
@@ -402,40 +410,38 @@ attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = threadIdx.x >> 7;
 
     griddep_launch_dependents();
-    if (threadIdx.x == 0) {
-        for (int t = 0; t < TILES; ++t) {
-            mbar_init(&q_full[t], 1);
-            mbar_init(&s_full[t], 1);
-            mbar_init(&s_read[t], 4);
-            mbar_init(&pv_done[t], 1);
-            mbar_init(&p_full[t][0], 4);
-            mbar_init(&p_full[t][1], 4);
-            mbar_init(&o_full[t], 1);
-        }
-        for (int i = 0; i < Cfg::kStages; ++i) { mbar_init(&full_bar[i], 1); mbar_init(&empty_bar[i], 1); }
-        mbar_init(&ragged_bar, 1);
-        *abort_flag = 0;
-        fence_mbar_init();
-    }
     if (warp == 4 * TILES) {
         tmem_alloc(tmem_slot, 256 * TILES);
         tmem_relinquish();
     }
     const AttnQuotient unit = attn_divide(blockIdx.x, p.s.heads, p.s.per_heads);
     const int head = unit.rest, kv_head = attn_divide(head, p.s.share, p.s.per_share).quotient;
-    // (sequences that the host knows are found beside the preceding kernel's end)
-    const bool known = !p.s.starts && !p.s.lengths;
-    if (!known) griddep_wait();
-    if (warp == 0) {
+    // the warp that loads sets the barriers up, a lane each, and has the first tiles on their way before the others go on
+    if (warp == 4 * TILES + 1) {
+        attn_barriers(sh.q_full, sh.s_read, 1);
+        attn_barriers(sh.s_read, sh.end, 4);
+        if (lane == 0) *abort_flag = 0;
+        fence_mbar_init();
+        griddep_wait();
         const AttnTile t = attn_locate<TILES * kAttnRows>(p.s, unit.quotient, p.s.causal);
         if (lane == 0) work = t;
+        __syncwarp();
+        if (t.len && elect_one()) {
+            const int q0 = t.tile * TILES * kAttnRows, c0 = attn_first_key_tile(p.s, q0) * kAttnRows;
+#pragma unroll
+            for (int v = 0; v < TILES; ++v)
+                if (q0 + v * kAttnRows < t.len) attn_load<HD>(smem + v * Cfg::kTile, &tmQ, &q_full[v], head, t.first + q0 + v * kAttnRows);
+            attn_load<HD>(ring, &tmK, &full_bar[0], kv_head, t.first + c0);
+            attn_load<HD>(ring + Cfg::kTile, &tmV, c0 + kAttnRows > t.len ? &ragged_bar : &full_bar[1], kv_head, t.first + c0);
+        }
+        __syncwarp();
     }
-    if (known) griddep_wait();
+    griddep_wait();
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
     // S of either tile, then O of either.  P: over the first and third quarter of S; where a head has 64 columns, behind O, so that the next scores wait
-    // for these ones to be read only (us, 4 x 4096 tokens, 16 heads: over / apart 384 / 340)
+    // for these ones to be read only (us, 4 x 4096 tokens, 16 heads, all tokens: over / apart 400 / 376)
     constexpr bool kApart = HD == 64;
     const uint32_t tmem = *tmem_slot;
     const uint32_t o_at = tmem + TILES * kAttnRows;
@@ -462,10 +468,12 @@ attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                 for (int j = begin; j < end && ok; ++j) {
 #pragma unroll
                     for (int v = 0; v < 2; ++v) {
-                        if (j == begin && v < tiles) attn_load<HD>(smem + v * Cfg::kTile, &tmQ, &q_full[v], head, first + q0 + v * kAttnRows);
-                        if (!attn_wait(&empty_bar[ps.stage], ps.phase ^ 1u, abort_flag)) { ok = false; break; }
-                        attn_load<HD>(ring + ps.stage * Cfg::kTile, v ? &tmV : &tmK, v && j == ragged ? &ragged_bar : &full_bar[ps.stage], kv_head,
-                                      first + j * kAttnRows);
+                        // (the first are on their way, and may be used and free again by now: nothing to wait for)
+                        if (j != begin) {
+                            if (!attn_wait(&empty_bar[ps.stage], ps.phase ^ 1u, abort_flag)) { ok = false; break; }
+                            attn_load<HD>(ring + ps.stage * Cfg::kTile, v ? &tmV : &tmK, v && j == ragged ? &ragged_bar : &full_bar[ps.stage], kv_head,
+                                          first + j * kAttnRows);
+                        }
                         ps.advance(Cfg::kStages);
                     }
                 }
@@ -803,8 +811,11 @@ __device__ __forceinline__ void attn_bwd_keys(const CUtensorMap& tmQ, const CUte
                     uint64_t* bars = rows_of(tile) < kAttnRows ? sh.ragged : sh.full;
 #pragma unroll
                     for (int g = 0; g < 2; ++g) {
-                        if (!attn_wait(&sh.empty[ps.stage], ps.phase ^ 1u, abort_flag)) { ok = false; break; }
-                        if (it) attn_load<HD>(ring + ps.stage * Cfg::kTile, g ? &tmdO : &tmQ, &bars[ps.stage], head, first + tile * kAttnRows);
+                        // (the first are on their way, and may be used and free again by now: nothing to wait for)
+                        if (it) {
+                            if (!attn_wait(&sh.empty[ps.stage], ps.phase ^ 1u, abort_flag)) { ok = false; break; }
+                            attn_load<HD>(ring + ps.stage * Cfg::kTile, g ? &tmdO : &tmQ, &bars[ps.stage], head, first + tile * kAttnRows);
+                        }
                         ps.advance(Cfg::kStages);
                     }
                     if (++tile == hi) { tile = lo; ++head; }

@@ -352,3 +352,20 @@ def test_more_blocks_than_fit_at_once(B, hd, heads, n):
     Q, K, V, dO = (t[2 * n:3 * n] for t in x)
     got = {name: t[:, 2 * n:3 * n] if name == "lse" else t[2 * n:3 * n] for name, t in a.items()}
     compare(got, Q, K, V, dO, hd, [(0, n)])
+
+
+@pytest.mark.parametrize("hd,n,causal", [(24, 333, True), (64, 384, False), (128, 200, True)])
+def test_small_calls_many_times(B, hd, n, causal):
+    """A few blocks whose first tiles are used up at once: no order of a block's warps may leave one of them waiting."""
+    import torch
+
+    Q, K, V, dO = tensors(n, 3, 3, hd, 28)
+    want = run(B, Q, K, V, dO, hd, causal=causal)
+    O, lse, grads = torch.empty_like(Q), torch.empty(3, n, device="cuda"), [torch.empty_like(x) for x in (Q, K, V)]
+    ws = torch.empty(B.slope_attention_bwd_workspace_bytes(n, 3, 3, hd), dtype=torch.uint8, device="cuda")
+    for _ in range(2000):
+        B.slope_attention_fwd(Q, K, V, hd, O, lse, causal=causal)
+        B.slope_attention_bwd(dO, Q, K, V, O, lse, hd, *grads, ws, causal=causal)
+    assert B.slope_poll_status() == 0
+    for name, x in zip(("O", "lse", "dQ", "dK", "dV"), (O, lse, *grads)):
+        assert torch.equal(x, want[name]), name
