@@ -351,10 +351,10 @@ def kernel_sources_sha256():
 # sources reports traffic = null (tests/test_bench_line.py fails until the capture is refreshed or
 # cleared).
 NCU_TRAFFIC = {
-    "sources": "942c5a0a6f01db870e8cdc616da4a50a50bc22c47b6f622e8ce3e3c80d78d6ee",
+    "sources": "b841e4cbbd34cc6a283f092a14f8fefae6c8315e65db602c910e40164d459f8e",
     "captured_tokens": 16384,
-    "sparse_bytes_per_launch": 496076709,     # mean over the 14 sparse GEMM launches of one step
-    "dense_bytes_per_launch": 768354523,     # mean over the 7 weight-gradient launches of one step
+    "sparse_bytes_per_launch": 495459785,     # mean over the 14 sparse GEMM launches of one step
+    "dense_bytes_per_launch": 795581550,     # mean over the 7 weight-gradient launches of one step
 }
 
 
