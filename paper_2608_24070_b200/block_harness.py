@@ -215,7 +215,8 @@ class _LayerNormFn(torch.autograd.Function):
 class Attention:
     """Softmax attention over the library's calls, behind the rotation of queries and keys by their positions if there are ``frequencies``
     (``binding.rotary_frequencies``).  A call takes the three projections' outputs [tokens x heads * head_dim] and says where the sequences lie;
-    ``positions`` int32 [tokens].  Rows of no sequence have an output and gradients of zero."""
+    ``positions`` int32 [tokens].  Rows of no sequence have an output and gradients of zero.  The backward pass is over the same sequences and
+    positions: these tensors and the frequencies must not be written in place before it (an error, as for any tensor that autograd keeps)."""
 
     def __init__(self, heads: int, kv_heads: Optional[int] = None, frequencies: Optional[torch.Tensor] = None, factor: float = 1.0,
                  interleaved: bool = False, causal: bool = True, window: int = 0, scale: Optional[float] = None):
@@ -236,29 +237,33 @@ class _AttentionFn(torch.autograd.Function):
         b, head_dim = q.shape[0], q.shape[1] // layer.heads
         if q.shape[1] % layer.heads or k.shape[1] != layer.kv_heads * head_dim:
             raise ValueError("Attention: the projections do not have these heads")
+        # (what the layer says now is what the backward pass goes by: another table, factor or mask is for the calls that follow)
+        frequencies, turn = layer.frequencies, {"factor": layer.factor, "interleaved": layer.interleaved}
         if positions is not None:
             turned = torch.empty_like(q, memory_format=torch.contiguous_format), torch.empty_like(k, memory_format=torch.contiguous_format)
-            B.slope_rotary(q, k, positions, layer.frequencies, head_dim, *turned, factor=layer.factor, interleaved=layer.interleaved)
+            B.slope_rotary(q, k, positions, frequencies, head_dim, *turned, **turn)
             q, k = turned
         # (rows of no sequence are not written)
         ctx.fresh = torch.empty if batch["starts"] is None and batch["lengths"] is None else torch.zeros
         O = ctx.fresh(b, layer.heads * head_dim, dtype=q.dtype, device=q.device)
         lse = torch.empty(layer.heads, b, dtype=torch.float32, device=q.device)
         B.slope_attention_fwd(q, k, v, head_dim, O, lse, **batch)
-        ctx.layer, ctx.batch, ctx.positions, ctx.head_dim = layer, batch, positions, head_dim
-        ctx.save_for_backward(q, k, v, O, lse)
+        starts, lengths = batch.pop("starts"), batch.pop("lengths")
+        ctx.batch, ctx.turn, ctx.sizes = batch, turn, (b, layer.heads, layer.kv_heads, head_dim)
+        # (where the sequences lie and the positions, too: one that is written before the backward pass is an error there, not other gradients)
+        ctx.save_for_backward(q, k, v, O, lse, starts, lengths, positions, frequencies)
         return O
 
     @staticmethod
     def backward(ctx, dO):
-        layer: Attention = ctx.layer
-        q, k, v, O, lse = ctx.saved_tensors
+        q, k, v, O, lse, starts, lengths, positions, frequencies = ctx.saved_tensors
+        head_dim = ctx.sizes[3]
         grads = [ctx.fresh(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v)]
-        workspace = _scratch(B.slope_attention_bwd_workspace_bytes(q.shape[0], layer.heads, layer.kv_heads, ctx.head_dim), q.device)
-        B.slope_attention_bwd(dO.contiguous(), q, k, v, O, lse, ctx.head_dim, *grads, workspace, **ctx.batch)
-        if ctx.positions is not None:
+        workspace = _scratch(B.slope_attention_bwd_workspace_bytes(*ctx.sizes), q.device)
+        B.slope_attention_bwd(dO.contiguous(), q, k, v, O, lse, head_dim, *grads, workspace, starts=starts, lengths=lengths, **ctx.batch)
+        if positions is not None:
             dq, dk = grads[:2]
-            B.slope_rotary(dq, dk, ctx.positions, layer.frequencies, ctx.head_dim, dq, dk, factor=layer.factor, interleaved=layer.interleaved, backward=True)
+            B.slope_rotary(dq, dk, positions, frequencies, head_dim, dq, dk, **ctx.turn, backward=True)
         return (*(_first_derivative(g, "Attention") for g in grads), None, None, None)
 
 
