@@ -138,7 +138,7 @@ __device__ __forceinline__ AttnTile attn_locate(const AttnShape& s, int unit, bo
             int first = 0, len = 0;
             if (i < s.sequences) {
                 first = min(max(s.starts[i], 0), s.b);
-                len = max(min(s.starts[i + 1], s.b) - first, 0);
+                len = max(min(max(s.starts[i + 1], 0), s.b) - first, 0);      // (both ends held first: the difference of any two ints need not be one)
                 if (s.lengths) len = min(len, max(s.lengths[i], 0));
             }
             const int own = (len + rows - 1) / rows;
