@@ -385,10 +385,12 @@ slope_status_t slope_rotary(const void* Q, int q_ld, const void* K, int k_ld, in
  *   lengths             int32 [sequences], device, or NULL: sequence i has no more than that many of its rows (a padded batch)
  *   causal, window      a token sees its own sequence, with causal != 0 itself and the tokens before it, with window > 0 (causal only) no more
  *                       than the last `window` of these, itself among them
- * Rows of no sequence are not written, and what they hold reaches no other row; a sequence may have length 0.  Starts are ascending and within
- * [0, b]; others are held to that range (no access is out of bounds, the results are not defined).  An infinity or a NaN shows in
+ * Rows of no sequence are not written, and what they hold reaches no other row; a sequence may have length 0.  The bits of a row of O and lse depend on
+ * its query and on the keys and values that it sees alone (with finite inputs: not on other queries, later tokens or the batch around it).  Starts are
+ * ascending and within [0, b]; others are held to that range (no access is out of bounds, the results are not defined).  An infinity or a NaN shows in
  * the rows that see it as the formula has it (a score of minus infinity is a probability of 0, one of plus infinity a row of NaN); one in V (for the
- * gradients: in any input) may also make rows NaN that have it in the same tile of 128 as their causal border or the end of their window.  Probabilities are rounded to bf16 for the second product; sums are fp32.  Outputs must not overlap inputs or one another.
+ * gradients: in any input) may also make rows NaN that have it in the same tile of 128 as their causal border or the end of their window.
+ * Probabilities are rounded to bf16 for the second product; sums are fp32.  Outputs must not overlap inputs or one another.
  */
 slope_status_t slope_attention_fwd(const void* Q, int q_ld, const void* K, int k_ld, const void* V, int v_ld, int b, int heads, int kv_heads,
                                    int head_dim, int sequences, const void* starts, const void* lengths, int causal, int window, float scale,

@@ -575,9 +575,11 @@ attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                 if (j != j_lo && !(ok = warp_wait(&pv_done[t], phase, abort_flag))) break;
                 tc_fence_after_sync();
             }
-            if (__any_sync(0xFFFFFFFFu, now > m + kAttnSlack)) {
-                const float next = fmaxf(m, now), part = next == m ? 1.0f : exp2_fast(m - next);
-                m = next;
+            // (a row moves its own m alone: its bits depend on no other row, be it of another sequence or of none; the vote is for the collective loads)
+            const bool ahead = now > m + kAttnSlack;
+            if (__any_sync(0xFFFFFFFFu, ahead)) {
+                const float part = ahead ? exp2_fast(m - now) : 1.0f;
+                m = ahead ? now : m;
                 l *= part;
 #pragma unroll 1
                 for (int c = 0; c < (j == j_lo ? 0 : p.s.head_dim); c += 32) {
