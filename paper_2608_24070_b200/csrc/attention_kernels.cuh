@@ -411,10 +411,11 @@ attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
     uint8_t* ring = smem + TILES * Cfg::kTile;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = threadIdx.x >> 7;
 
-    griddep_launch_dependents();
+    // (behind the allocation: a dependent block that took the tensor memory first would wait for this grid, and this block for the memory)
     if (warp == 4 * TILES) {
         tmem_alloc(tmem_slot, 256 * TILES);
         tmem_relinquish();
+        griddep_launch_dependents();
     }
     const AttnQuotient unit = attn_divide(blockIdx.x, p.s.heads, p.s.per_heads);
     const int head = unit.rest, kv_head = attn_divide(head, p.s.share, p.s.per_share).quotient;
@@ -760,7 +761,6 @@ __device__ __forceinline__ void attn_bwd_keys(const CUtensorMap& tmQ, const CUte
     uint8_t *sK = smem, *sV = smem + Cfg::kTile, *ring = smem + 2 * Cfg::kTile;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = threadIdx.x >> 7;
 
-    griddep_launch_dependents();
     if (threadIdx.x < 8) {
         sh.ones[threadIdx.x] = make_uint4(0x3F803F80u, 0x00003F80u, 0u, 0u);
         fence_proxy_async_smem();
@@ -768,6 +768,7 @@ __device__ __forceinline__ void attn_bwd_keys(const CUtensorMap& tmQ, const CUte
     if (warp == 8) {
         tmem_alloc(&sh.tmem, 512);
         tmem_relinquish();
+        griddep_launch_dependents();          // (behind the allocation, as in the forward pass)
     }
     const AttnQuotient unit = attn_divide(block, p.s.kv_heads, p.s.per_kv_heads);
     const int kv_head = unit.rest, share = p.s.share;
@@ -1033,10 +1034,10 @@ __device__ __forceinline__ void attn_bwd_queries(const CUtensorMap& tmQ, const C
     uint8_t *sQ = smem, *sdO = smem + Cfg::kTile, *keys = smem + 2 * Cfg::kTile, *values = keys + Cfg::kKeys * Cfg::kTile;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = threadIdx.x >> 7;
 
-    griddep_launch_dependents();
     if (warp == 8) {
         tmem_alloc(&sh.tmem, 512);
         tmem_relinquish();
+        griddep_launch_dependents();          // (behind the allocation, as in the forward pass)
     }
     const AttnQuotient unit = attn_divide(block, p.s.heads, p.s.per_heads);
     const int head = unit.rest, kv_head = attn_divide(head, p.s.share, p.s.per_share).quotient;
