@@ -41,6 +41,14 @@ static slope_status_t attn_batch(AttnShape* s, int b, int heads, int kv_heads, i
                    static_cast<float>(kv_heads) / heads};
     return SLOPE_OK;
 }
+// Keys that a query of a sequence sees, in the mean; with starts or lengths, which only the device knows, as if the sequences shared the rows evenly.
+// (Causal, window w of n tokens: w - w^2 / 2 n, and n / 2 without a window or with one that leaves nothing out.)
+static double attn_reach(const AttnShape& s) {
+    const double n = s.part;
+    if (!s.causal || s.part == 0) return n;
+    const double w = s.window ? std::min<double>(s.window, n) : n;
+    return w * (1.0 - w / (2.0 * n));
+}
 template <typename Kernel, typename... Args>
 static slope_status_t launch_attn(Kernel kern, long long grid, int threads, int smem, cudaStream_t stream, const Args&... args) {
     if (!set_smem(kern, smem)) return SLOPE_ERR_CUDA;
@@ -98,7 +106,9 @@ slope_status_t slope_attention_fwd(const void* Q, int q_ld, const void* K, int k
     //   heads of 64, 16384 tokens, 16 heads: 16 x 1024 causal 82 / 94, 4 x 4096 causal 206 / 211, 8 x 2048 full 196 / 196, 4 x 4096 full 386 / 372
     //   heads of 128, 16384 tokens, 8 heads: 64 x 256 causal 36 / 42, 16 x 1024 causal 59 / 60, 8 x 2048 causal 90 / 89, 4 x 4096 full 300 / 282
     //   1024 tokens alone, causal: 16 heads of 64 16.5 / 19.3, 8 heads of 128 21.7 / 24.9
-    const int reach = p.s.window ? std::min(p.s.window, p.s.part) : causal ? p.s.part / 2 : p.s.part;  // keys of a query, in the mean
+    //   windows of 4096 tokens' sequences, 64 columns: 3000 (reach 1901) 193 / 204, 1024 (896) 113 / 127; 128 columns: 3000 148 / 145, 1024 86 / 90,
+    //   512 (480) 65 / 69; of 1024 tokens' sequences, 128 columns: 700 (461) 59 / 62
+    const double reach = attn_reach(p.s);
     const bool one = reach <= (head_dim <= 64 ? 2048 : 512) || attn_units(b, sequences, p.s.starts, 2 * kAttnRows) * heads <= info.sm_count;
     if (head_dim <= 64) return one ? attn_fwd<64, 1>(p, tm, stream) : attn_fwd<64, 2>(p, tm, stream);
     return one ? attn_fwd<128, 1>(p, tm, stream) : attn_fwd<128, 2>(p, tm, stream);
