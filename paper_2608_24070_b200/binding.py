@@ -357,7 +357,8 @@ def slope_dense_linear_bwd_dw_q8(dY, X_ckpt, dW, workspace=None):
 
 def slope_rotary(Q, K, positions, frequencies, head_dim, Qr, Kr, factor=1.0, interleaved=False, backward=False):
     """Qr, Kr: queries and keys turned by their positions (backward: gradients turned back).  K and Kr may be None; Qr and Kr may be Q and K.
-    Rows may be further apart than they are long (columns of a wider matrix), here and in the attention calls."""
+    Rows may be further apart than they are long (columns of a wider matrix), here and in the attention calls; positions, frequencies, starts, lengths
+    and the lse of the backward pass may be parts of longer vectors (one that does not begin on 16 bytes goes in as a copy)."""
     st = (_native or _calls()).slope_rotary(Q, K, positions, frequencies, head_dim, Qr, Kr, factor, interleaved, backward)
     if st:
         _check("slope_rotary", st)

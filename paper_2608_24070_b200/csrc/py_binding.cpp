@@ -437,6 +437,17 @@ void same(const Rows& a, const Rows& like) {
     if (a.type != like.type) refuse(PyExc_TypeError, "tensor of the wrong type");
     if (a.rows != like.rows || a.cols != like.cols) refuse(PyExc_ValueError, "tensor of the wrong shape");
 }
+// A vector (or matrix) that is read value by value: part of a longer one, from any element on.  The C ABI asks for 16 bytes of every base pointer, so
+// what begins elsewhere goes in as a copy (torch's, on the stream of the call; its memory is free for later work of that stream when the call is out).
+struct Values {
+    at::Tensor copy;
+    void* at;
+    Values(const at::Tensor* t, int64_t rows, int64_t cols, at::ScalarType type) : at(checked(t, rows, cols, type)) {
+        if ((reinterpret_cast<uintptr_t>(at) & 15) == 0) return;
+        copy = t->detach().clone();
+        at = copy.data_ptr();
+    }
+};
 int heads_of(const Rows& m, int head_dim) {
     if (head_dim < 1 || m.cols % head_dim != 0) refuse(PyExc_ValueError, "the columns are no whole number of heads");
     return extent(m.cols / head_dim);
@@ -458,26 +469,22 @@ SLOPE_PY(slope_rotary) {
             if (K.rows != Q.rows) refuse(PyExc_ValueError, "tensor of the wrong shape");
         }
         if (frequencies.dim() != 1) refuse(PyExc_ValueError, "tensor of the wrong shape");
-        void *pos = checked(&positions, 0, Q.rows, at::kInt), *freq = checked(&frequencies, 0, frequencies.size(0), at::kDouble);
+        const Values pos(&positions, 0, Q.rows, at::kInt), freq(&frequencies, 0, frequencies.size(0), at::kDouble);
         return call(p_slope_rotary, Q.at, Q.ld, K.at, K.ld, Q.type == at::kFloat ? SLOPE_F32 : SLOPE_BF16, extent(Q.rows), heads_of(Q, head_dim),
-                    K.at ? heads_of(K, head_dim) : 0, head_dim, extent(2 * frequencies.size(0)), interleaved, backward, pos, freq, factor, Qr.at, Qr.ld,
+                    K.at ? heads_of(K, head_dim) : 0, head_dim, extent(2 * frequencies.size(0)), interleaved, backward, pos.at, freq.at, factor, Qr.at, Qr.ld,
                     Kr.at, Kr.ld);
     });
 }
 // What both attention calls take of a batch.
 struct Batch {
-    int sequences, causal, window;
-    void *starts, *lengths;
+    int sequences;
+    const at::Tensor *s, *l;
+    int causal, window;
     float scale;
-    explicit Batch(Args& a) {
-        sequences = a.integer();
-        const at::Tensor *s = a.tensor_or_none(), *l = a.tensor_or_none();
-        causal = a.integer();
-        window = a.integer();
-        scale = a.number();
-        starts = checked(s, 0, static_cast<int64_t>(sequences) + 1, at::kInt);
-        lengths = checked(l, 0, sequences, at::kInt);
-    }
+    Values starts, lengths;
+    explicit Batch(Args& a)
+        : sequences(a.integer()), s(a.tensor_or_none()), l(a.tensor_or_none()), causal(a.integer()), window(a.integer()), scale(a.number()),
+          starts(s, 0, static_cast<int64_t>(sequences) + 1, at::kInt), lengths(l, 0, sequences, at::kInt) {}
 };
 void attention_operands(const Rows& Q, const Rows& K, const Rows& V) {
     if (Q.type != at::kBFloat16 || K.type != at::kBFloat16) refuse(PyExc_TypeError, "tensor of the wrong type");
@@ -494,8 +501,8 @@ SLOPE_PY(slope_attention_fwd) {
         attention_operands(Q, K, V);
         same(O, Q);
         const int heads = heads_of(Q, head_dim), kv_heads = heads_of(K, head_dim);
-        return call(p_slope_attention_fwd, Q.at, Q.ld, K.at, K.ld, V.at, V.ld, extent(Q.rows), heads, kv_heads, head_dim, s.sequences, s.starts, s.lengths,
-                    s.causal, s.window, s.scale, O.at, O.ld, checked(lse, heads, Q.rows, at::kFloat));
+        return call(p_slope_attention_fwd, Q.at, Q.ld, K.at, K.ld, V.at, V.ld, extent(Q.rows), heads, kv_heads, head_dim, s.sequences,
+                    s.starts.at, s.lengths.at, s.causal, s.window, s.scale, O.at, O.ld, checked(lse, heads, Q.rows, at::kFloat));
     });
 }
 SLOPE_PY(slope_attention_bwd) {
@@ -513,9 +520,9 @@ SLOPE_PY(slope_attention_bwd) {
         same(dK, K);
         same(dV, K);
         const int heads = heads_of(Q, head_dim), kv_heads = heads_of(K, head_dim);
-        return call(p_slope_attention_bwd, dO.at, dO.ld, Q.at, Q.ld, K.at, K.ld, V.at, V.ld, O.at, O.ld, checked(&lse, heads, Q.rows, at::kFloat),
-                    extent(Q.rows), heads, kv_heads, head_dim, s.sequences, s.starts, s.lengths, s.causal, s.window, s.scale, dQ.at, dQ.ld, dK.at,
-                    dK.ld, dV.at, dV.ld, ws.at, ws.bytes);
+        const Values logs(&lse, heads, Q.rows, at::kFloat);
+        return call(p_slope_attention_bwd, dO.at, dO.ld, Q.at, Q.ld, K.at, K.ld, V.at, V.ld, O.at, O.ld, logs.at, extent(Q.rows), heads,
+                    kv_heads, head_dim, s.sequences, s.starts.at, s.lengths.at, s.causal, s.window, s.scale, dQ.at, dQ.ld, dK.at, dK.ld, dV.at, dV.ld, ws.at, ws.bytes);
     });
 }
 
