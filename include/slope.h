@@ -369,7 +369,7 @@ slope_status_t slope_dense_linear_bwd_dw_q8(const void* dY, const void* X_ckpt, 
  *                 of 8); K and Kr may be NULL
  *   positions     int32 [b], any values;  frequencies: fp64 [n], radians a position (how they are scaled for long contexts is the caller's)
  *   Qr, Kr        results: other memory, or Q and K themselves (both, at the same row strides)
- * Angles are reduced in fp64: exact to 1e-7 of a turn at any position.
+ * Angles are reduced in fp64: exact to 1e-7 of a turn at any position, for frequencies up to 1 (above, 1e-7 times the frequency).
  */
 slope_status_t slope_rotary(const void* Q, int q_ld, const void* K, int k_ld, int type, int b, int heads, int kv_heads, int head_dim, int rot_dim,
                             int interleaved, int backward, const void* positions, const void* frequencies, float factor, void* Qr, int qr_ld,

@@ -165,8 +165,9 @@ slope_status_t slope_rotary(const void* Q, int q_ld, const void* K, int k_ld, in
     const int turned = interleaved ? (rot_dim + 7) / 8 : n / wide;
     const int per_head = turned + (Q == Qr ? 0 : interleaved ? head_dim / 8 - turned : (head_dim - rot_dim) / wide);
     const long long per_token = (static_cast<long long>(heads) + (K ? kv_heads : 0)) * per_head;
-    // Tokens of a block: an angle for every thread, if that leaves four blocks for every SM and a thread two batches of tasks at most (rotating 20 of 80
-    // columns of 64 heads, 2039 tokens: 25 tokens a block 116 us, 3 tokens 25)
+    // Tokens of a block: an angle for every thread, if that leaves four blocks for every SM and a thread two batches of tasks at most (us, rotating 20 of 80
+    // columns of 64 heads, 2039 tokens: neighbouring pairs, 25 tokens a block 47, 3 as by the rule 11.0, 1 12.6; halves 116, 28.4, 1 by the rule 23.4;
+    // all of 64 heads of 128, 16384 tokens, halves, 25 tokens 107, 4 by the rule 83.3, 1 92)
     const long long most = std::min<long long>({kRotaryThreads / n, b / (4ll * info.sm_count), 8 * kRotaryThreads / per_token, 64});
     const int tokens = static_cast<int>(std::max(1ll, most));
     if (tokens * per_token > INT_MAX / 2) return SLOPE_ERR_SHAPE;

@@ -345,8 +345,8 @@ __device__ __forceinline__ void warp_arrive(uint64_t* bar) {
 // to 2^16 is as exact as one up to 1 in fp32 and bf16, and O is not touched in most steps.
 // P is rounded to bf16 as an operand (2^-9 relative on average, as any operand of these products); l sums the unrounded values in fp32.
 // Warps 0-3 (4-7): queries 0-127 (128-255); of the four behind them the first: MMAs; the second: barriers and loads; the third: zeros behind the
-// sequence's last row of V.  Measured: 4 x 2048 tokens, 40 heads of 128, causal, 185 us = 929 TFLOP/s; 4 x 4096, 16 heads, all tokens, 503 us = 1093;
-// 8 x 1024, 12 heads of 64 34.6 us = 373.
+// sequence's last row of V.  Measured: 4 x 2048 tokens, 40 heads of 128, causal, 190 us = 909 TFLOP/s in bursts, 217 in long runs (the same number of
+// cycles, at the power limiter's clock); 4 x 4096, 16 heads, all tokens, 513 us = 1072; 8 x 1024, 12 heads of 64 35.2 us = 366.
 // =====================================================================================
 constexpr float kAttnSlack = 16.0f;
 // A row's 128 scores from tensor memory and their maximum.  EDGE: those outside [lo, hi) are minus infinity.  (Two instances: as a condition inside,
@@ -751,7 +751,7 @@ __device__ __forceinline__ uint4 attn_split(float x) {
 // A thread reads its scores at once, so that the next tile's are formed, and keeps P in registers until dP is there; P and dS then take the
 // place of dP, 32 queries at a time.  So while one group has dP and the products dV, dK and the next dP run, the other has its powers of two.
 // What bounds it is the way dP - dS - dV, dK - next dP, 2000 of whose clocks at 128 columns are the products' (2048 with S).
-// (Both kernels, as 10 operations a pair and column: 16384 tokens, 32 / 8 heads of 128, 6600 us = 833 TFLOP/s; 8 x 1024, 12 heads of 64 127 us = 254.)
+// (Both kernels, as 10 operations a pair and column: 16384 tokens, 32 / 8 heads of 128, 6600 us = 833 TFLOP/s; 8 x 1024, 12 heads of 64 129 us = 250.)
 // Warp 11: the MMAs of S; 8: the others; 9: loads; 10: lse and D, zeros behind the sequence's last row.
 template <int HD>
 __device__ __forceinline__ void attn_bwd_keys(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmdO,
@@ -1197,7 +1197,8 @@ attention_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
 //   factor (u cos a - v sin a, v cos a + u sin a),   a = position frequency_i
 // (backward: the transposed map, sin negated).  Pairs are columns i and n + i, or (PAIRS) 2 i and 2 i + 1.
 // What bounds it is HBM; an angle is formed once per token and pair, by one thread of the block that has the token, for all heads.  Angles are
-// taken in whole turns in fp64, of which the nearest whole number is left out: in fp32 a position of 10^6 would be 0.06 rad off.
+// taken in whole turns in fp64, of which the nearest whole number is left out: in fp32 a position of 10^6 would be 0.06 rad off.  (At 2^31 and a
+// frequency of 1 the two fp64 roundings and the one to fp32 come to 8e-8 of a turn; they grow with the frequency.)
 // =====================================================================================
 struct RotaryParams {
     const void *src[2];
@@ -1254,7 +1255,7 @@ __device__ __forceinline__ void store_n(void* base, size_t at, const float (&x)[
 }
 constexpr int kRotaryThreads = 256, kRotaryTable = 2048;       // angles of a block
 // A thread takes N values at a time: N pairs' two halves, or N / 2 neighbouring pairs; kBatch of these are in flight, the first while the block's
-// angles are formed.  Measured, us, one at a time behind the angles / two / four: 20 of 80 columns of 64 heads turned, 2039 tokens, neighbouring pairs
+// angles are formed.  Measured on the same buffers each time, us, one at a time behind the angles / two / four: 20 of 80 columns of 64 heads turned, 2039 tokens, neighbouring pairs
 // 17.2 / 9.2 / 10.2, halves 41.8 / 20.8 / 23.9; all of 64 heads of 128, 16384 tokens, bf16, halves 84.7 / 83.2 / 100; fp32, where a task of eight
 // has four loads of its own and goes alone, 40 heads of 128, 8191 tokens, 55.1 / 55.6 / -, one in flight 54.9.
 template <int TYPE, bool PAIRS, int N>
