@@ -251,7 +251,9 @@ class _AttentionFn(torch.autograd.Function):
         starts, lengths = batch.pop("starts"), batch.pop("lengths")
         ctx.batch, ctx.turn, ctx.sizes = batch, turn, (b, layer.heads, layer.kv_heads, head_dim)
         # (where the sequences lie and the positions, too: one that is written before the backward pass is an error there, not other gradients)
-        ctx.save_for_backward(q, k, v, O, lse, starts, lengths, positions, frequencies)
+        # (autograd keeps no tensor of inference mode: a table that was made in it, as evaluation does, goes in as a copy)
+        kept = (t.clone() if t is not None and t.is_inference() else t for t in (starts, lengths, positions, frequencies))
+        ctx.save_for_backward(q, k, v, O, lse, *kept)
         return O
 
     @staticmethod

@@ -93,3 +93,17 @@ def test_two_passes_forward_with_buffers_of_their_own(calls):
         assert torch.equal(batch["lengths"], used["lengths"]) and torch.equal(batch["starts"], used["starts"])
     for (args, _), used in zip(calls["slope_rotary"][2:], (other, where)):
         assert torch.equal(args[2], used["positions"])
+
+
+def test_tables_made_in_inference_mode(calls):
+    """Positions and frequencies that an evaluation left behind, then a training step; and no graph at all."""
+    with torch.inference_mode():
+        attention, _, where = made()
+        attention(*(torch.zeros(ROWS, n * HD, dtype=torch.bfloat16) for n in (HEADS, KV, KV)), **where)
+    _, x, _ = made()
+    attention(*x, **where).float().sum().backward()
+    forward, backward = calls["slope_rotary"][1:]
+    assert torch.equal(forward[0][2], backward[0][2]) and torch.equal(forward[0][3], backward[0][3])
+    assert torch.equal(calls["slope_attention_bwd"][0][1]["starts"], where["starts"])
+    with torch.no_grad():
+        attention(*x, **where)
